@@ -376,6 +376,174 @@ HYQ_API int hyq_decode_attn(const hyq_dcache* cache, const void* q, float softma
 HYQ_API int hyq_decode_attn_noalloc(const hyq_dcache* cache, const void* q, float softmax_scale,
                                     void* out, int32_t out_dtype, void* stream);
 
+/* ======================================================================
+ * Paged serving: the calls that stand before and beside the ones above in a
+ * server of many sequences.
+ *
+ *   hyq_norm_rope     per-head RMS norms of queries and keys and the position
+ *                     rotation in one pass, from token-major projections to
+ *                     the [B][H][L][D] tensors of the prefill and decode calls;
+ *   hyq_paged_append  the same pass for the new tokens of a ragged batch; keys
+ *                     and values go into the pages of a cache;
+ *   hyq_paged_attn    causal attention of each sequence's new tokens (one, a
+ *                     few, or a chunk) over its pages; on request, the
+ *                     attention weight that every cached key received;
+ *   hyq_evict         eviction by that weight, per KV head, into new pages.
+ *
+ * A paged cache is a pool of n_pages pages of `page` slots for each of the
+ * Hkv heads.  A sequence owns the pages that its row of a block table lists:
+ * its slot n is slot n % page of page table[n / page].  One table serves all
+ * heads.  Keys and values are rows of D channels, bf16, or 8-bit codes with
+ * one float32 scale per row (s = max|x| / c, code = the value nearest to
+ * fl32(x / s), c = 127 for int8 and 448 for E4M3, rounding as at
+ * hyq_quantize; s = 0 gives codes 0).
+ *
+ * What a device array says is not checked on the host, but bounded in the
+ * kernels: a table entry outside [0, n_pages) is a hole, whose keys nobody
+ * sees and whose rows are not written; lengths are taken as at most the
+ * bounds given with them.  No such value makes a kernel leave its buffers.
+ * Slots behind a sequence may hold anything (NaN too); the rows of its own
+ * slots must be finite.  Buffers must be aligned to 16 bytes.
+ * ==================================================================== */
+
+typedef struct hyq_rope {
+  int32_t rot_dim;        /* channels [0, rot_dim) are rotated: a multiple of 16, 0..D */
+  int32_t interleaved;    /* pairs of frequency f: 0 channels (f, f + rot_dim/2),
+                             1 channels (2f, 2f + 1)                              */
+  float eps;              /* added to the mean square, >= 0                       */
+  const void* q_weight;   /* bf16 [D], NULL: queries are not normalized           */
+  const void* k_weight;   /* bf16 [D], NULL: keys are not normalized              */
+  const float* inv_freq;  /* [rot_dim/2] radians per position (not read if rot_dim = 0) */
+} hyq_rope;
+
+/*
+ * For every row x of q (weight w = q_weight) and k (k_weight):
+ *   y = x * w / sqrt(mean(x^2) + eps)        (y = x where w is NULL)
+ *   the pair (a, c) of frequency f becomes (a cos - c sin, c cos + a sin) of
+ *   the angle pos * inv_freq[f]
+ * in float32 (the angle in float64), rounded to bf16 once; v is copied.
+ * Token t = b * L + i of shape (its B, Hq, Hkv, L, D count here; the other
+ * fields only have to be valid).  q: bf16 rows [B*L][Hq][D] with q_stride
+ * elements from token to token (a multiple of 8, >= Hq * D), k and v the same
+ * with Hkv heads (three slices of one packed projection, or three tensors).
+ * pos: int32 [B*L], any value.  Q [B][Hq][L][D], K and V [B][Hkv][L][D] bf16,
+ * not overlapping the inputs.  v and V may be NULL together; so may k and K.
+ * With L = 1 the outputs are the rows of hyq_decode_append / hyq_decode_attn.
+ */
+HYQ_API int hyq_norm_rope(const hyq_shape* shape, const hyq_rope* rope, const void* q,
+                          int64_t q_stride, const void* k, int64_t k_stride, const void* v,
+                          int64_t v_stride, const int32_t* pos, void* Q, void* K, void* V,
+                          void* stream);
+
+typedef struct hyq_pcache {
+  int32_t Hq, Hkv, D;    /* query heads that read it, KV heads, head dim (128)     */
+  int32_t page;          /* slots per page: 16, 32, 64, 128 or 256                 */
+  int32_t n_pages;       /* pages in the pool                                      */
+  int32_t bits_kv;       /* 16 (bf16) or 8                                         */
+  int32_t kv_format;     /* 8 bits: HYQ_FMT_INT or HYQ_FMT_FP8                     */
+  /* caller-owned device buffers (byte sizes from hyq_pcache_init) */
+  void* k;               /* [n_pages][Hkv][page][D] bf16 or code bytes             */
+  void* v;               /* the same                                               */
+  float* k_scale;        /* [n_pages][Hkv][page], 8 bits only                      */
+  float* v_scale;
+  float* mass;           /* [n_pages][Hkv][page] attention weight received; NULL if
+                            nobody collects it                                     */
+} hyq_pcache;
+
+typedef struct hyq_pcache_sizes {
+  size_t kv_bytes;       /* of k and of v                                          */
+  size_t scale_bytes;    /* of k_scale and of v_scale (0 with 16 bits)             */
+  size_t mass_bytes;     /* of mass                                                */
+} hyq_pcache_sizes;
+
+/* One step of B sequences with T token rows in all: tokens [cu_new[b],
+   cu_new[b+1]) are the new ones of sequence b (none is fine), which go to its
+   slots lens[b], lens[b] + 1, ...  Rows from cu_new[B] on belong to nobody:
+   they are neither read nor written.  A page that the step writes (its new
+   slots, or mass) must belong to one sequence only; pages that are only read
+   may be shared.                                                            */
+typedef struct hyq_pbatch {
+  int32_t B, T;
+  int32_t max_new;         /* no sequence has more new tokens                      */
+  int32_t max_len;         /* no lens[b] is larger                                 */
+  int32_t max_pages;       /* entries per table row                                */
+  const int32_t* cu_new;   /* device [B + 1], ascending from 0                     */
+  const int32_t* lens;     /* device [B]: slots in use before the step             */
+  const int32_t* table;    /* device [B][max_pages]                                */
+} hyq_pbatch;
+
+/* Pure host arithmetic: checks the geometry, fills it in (buffers NULL) and
+   returns the buffer sizes (sizes may be NULL).                              */
+HYQ_API int hyq_pcache_init(int32_t Hq, int32_t Hkv, int32_t D, int32_t page, int32_t n_pages,
+                            int32_t bits_kv, int32_t kv_format, hyq_pcache* cache,
+                            hyq_pcache_sizes* sizes);
+
+/*
+ * hyq_norm_rope for the new tokens of a batch: q rows to q_out [T][Hq][D]
+ * bf16, k and v rows into their slots (codes are taken of the float32 values,
+ * not of bf16 ones); mass, where there is one, is 0 in those slots.
+ * q, k, v: bf16 rows [T][heads][D] with strides as for hyq_norm_rope; pos
+ * int32 [T].  q and q_out may be NULL together (keys and values only).
+ * lens is not changed: hyq_paged_attn of the same step takes the same batch.
+ */
+HYQ_API int hyq_paged_append(const hyq_pcache* cache, const hyq_pbatch* batch,
+                             const hyq_rope* rope, const void* q, int64_t q_stride, const void* k,
+                             int64_t k_stride, const void* v, int64_t v_stride,
+                             const int32_t* pos, void* q_out, void* stream);
+
+#define HYQ_MASS_NONE 0   /* the weights are not collected                         */
+#define HYQ_MASS_ADD  1   /* added to cache.mass                                   */
+#define HYQ_MASS_SET  2   /* cache.mass = the weights of this call                 */
+
+/* Workspace of hyq_paged_attn for this cache and these bounds (host only; the
+   device arrays of the batch are not read and may be NULL).  0: none needed. */
+HYQ_API int hyq_paged_ws_bytes(const hyq_pcache* cache, const hyq_pbatch* batch, int32_t mass,
+                               size_t* bytes);
+
+/*
+ * For new token i of sequence b, query head h and its KV head j:
+ *   z_n = softmax_scale * <q, K[n]> over the slots n <= lens[b] + i,
+ *   out = sum_n w_n V[n] / sum_n w_n, w_n = exp(z_n - max z);
+ * a row that sees no key (all holes) gives 0.  The new tokens' rows must be
+ * in their slots (hyq_paged_append).
+ * With mass, for every slot n < lens[b] + new of a sequence with new tokens:
+ *   mass[b][j][n] (+)= sum over its new tokens i and the g heads of group j of
+ *                      the weight w_n / sum w that they give n.
+ * q: bf16 [T][Hq][D]; out: [T][Hq][D], float32 (out_dtype 0) or bf16 (1).
+ * Precision: bf16 products (8-bit codes are exact in bf16, their scales are
+ * applied in float32), float32 sums; the weights enter the products with V as
+ * a high + low bf16 pair where a sequence has at most 16 query rows per KV
+ * head (new tokens * Hq/Hkv), and as bf16 where it has more.  Every result is
+ * the same from run to run: nothing is added atomically.
+ * Allocates nothing and keeps no state; it can be captured in a HIP graph
+ * (lens, tables and token counts may change between replays, within the
+ * bounds).  ws: scratch of hyq_paged_ws_bytes; calls that overlap need one each.
+ */
+HYQ_API int hyq_paged_attn(const hyq_pcache* cache, const hyq_pbatch* batch, const void* q,
+                           float softmax_scale, int32_t mass, void* out, int32_t out_dtype,
+                           void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * Eviction by accumulated attention weight.  Of the n = min(lens[b], max_len)
+ * slots of sequence b, every KV head keeps min(n, budget): the last `recent`
+ * ones, and of the others those with the largest cache.mass (ties: the lowest
+ * slot; -0 equals +0, NaN counts as less than any number), in ascending order:
+ *   keep[b][j][i] = the i-th kept slot (entries i >= min(n, budget) hold
+ *                   HYQ_KQ_POS_PAD),
+ * whose key, value, scales and mass go to slot i of the pages of row b of
+ * new_table; new_lens[b] = min(n, budget).  Slots behind that are left as they
+ * were, and so are the old pages: the caller may free them.  The new pages
+ * must be no one else's, old pages of this call among them.  Old pages may be
+ * shared (by sequences, or with readers).
+ * B sequences; table int32 [B][max_pages], new_table int32 [B][new_pages] with
+ * new_pages * page >= budget >= recent >= 0, budget >= 1; keep int32
+ * [B][Hkv][budget], new_lens int32 [B] (another array than lens).
+ */
+HYQ_API int hyq_evict(const hyq_pcache* cache, int32_t B, const int32_t* lens,
+                      const int32_t* table, int32_t max_pages, int32_t max_len, int32_t budget,
+                      int32_t recent, const int32_t* new_table, int32_t new_pages, int32_t* keep,
+                      int32_t* new_lens, void* stream);
+
 /* Static description of a return code. */
 HYQ_API const char* hyq_strerror(int code);
 

@@ -1,6 +1,6 @@
 """Python binding of libhyq, the MI355X (gfx950) HyQuant hybrid-precision
-attention library (prefill operator, and the decode cache with its
-attention).
+attention library (prefill operator, the decode cache with its attention, and
+the paged serving calls: norms and rotation, paged attention, eviction).
 
 The functions here carry the C ABI's names (``include/hyq.h``) and only
 marshal arguments: torch tensors (device memory) become pointers, the
@@ -26,10 +26,13 @@ KQ_POS_PAD = 0x7FFFFFFF
 FMT_INT, FMT_FP8, FMT_FP4, FMT_FP4Q6 = 0, 1, 2, 3   # hyq_shape.kv_format
 WIN_FIXED, WIN_BAND = 0, 1    # hyq_shape.window_mode
 SEL_PROXY, SEL_COLMASS = 0, 1  # hyq_shape.selector
+MASS_NONE, MASS_ADD, MASS_SET = 0, 1, 2   # what hyq_paged_attn does with the weights
 DECODE_WS = 64                # HYQ_DECODE_WS: staging buffer capacity
 EXPORTED = ("hyq_sizes_for", "hyq_select_vertical", "hyq_quantize", "hyq_attn_prefill",
             "hyq_prefill", "hyq_strerror", "hyq_last_error", "hyq_dcache_init", "hyq_freeze",
-            "hyq_decode_append", "hyq_decode_attn", "hyq_decode_attn_noalloc")
+            "hyq_decode_append", "hyq_decode_attn", "hyq_decode_attn_noalloc", "hyq_norm_rope",
+            "hyq_pcache_init", "hyq_paged_append", "hyq_paged_ws_bytes", "hyq_paged_attn",
+            "hyq_evict")
 
 
 class HyqError(RuntimeError):
@@ -68,6 +71,30 @@ _DSIZES = ("k_codes_bytes", "v_codes_bytes", "k_scale_bytes", "v_scale_bytes", "
 
 class _DCacheSizes(ctypes.Structure):
     _fields_ = [(n, ctypes.c_size_t) for n in _DSIZES]
+
+
+class _Rope(ctypes.Structure):
+    _fields_ = [("rot_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32),
+                ("eps", ctypes.c_float), ("q_weight", ctypes.c_void_p),
+                ("k_weight", ctypes.c_void_p), ("inv_freq", ctypes.c_void_p)]
+
+
+_PCACHE_INTS = ("Hq", "Hkv", "D", "page", "n_pages", "bits_kv", "kv_format")
+_PCACHE_PTRS = ("k", "v", "k_scale", "v_scale", "mass")
+
+
+class _PCache(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in _PCACHE_INTS] + \
+               [(n, ctypes.c_void_p) for n in _PCACHE_PTRS]
+
+
+class _PCacheSizes(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_size_t) for n in ("kv_bytes", "scale_bytes", "mass_bytes")]
+
+
+class _PBatch(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("B", "T", "max_new", "max_len", "max_pages")] + \
+               [(n, ctypes.c_void_p) for n in ("cu_new", "lens", "table")]
 
 
 @dataclasses.dataclass(frozen=True)
@@ -123,6 +150,17 @@ def lib():
         L.hyq_decode_attn.argtypes = [DC, P, ctypes.c_float, P, ctypes.c_int32, P,
                                       ctypes.c_size_t, P]
         L.hyq_decode_attn_noalloc.argtypes = [DC, P, ctypes.c_float, P, ctypes.c_int32, P]
+        I32, I64 = ctypes.c_int32, ctypes.c_int64
+        RP, PC, PB = ctypes.POINTER(_Rope), ctypes.POINTER(_PCache), ctypes.POINTER(_PBatch)
+        L.hyq_norm_rope.argtypes = [ctypes.POINTER(_Shape), RP, P, I64, P, I64, P, I64] + [P] * 5
+        L.hyq_pcache_init.argtypes = [I32] * 7 + [PC, ctypes.POINTER(_PCacheSizes)]
+        L.hyq_paged_append.argtypes = [PC, PB, RP, P, I64, P, I64, P, I64, P, P, P]
+        L.hyq_paged_ws_bytes.argtypes = [PC, PB, I32, ctypes.POINTER(ctypes.c_size_t)]
+        L.hyq_paged_attn.argtypes = [PC, PB, P, ctypes.c_float, I32, P, I32, P, ctypes.c_size_t, P]
+        L.hyq_evict.argtypes = [PC, I32, P, P, I32, I32, I32, I32, P, I32, P, P, P]
+        for f in ("hyq_norm_rope", "hyq_pcache_init", "hyq_paged_append", "hyq_paged_ws_bytes",
+                  "hyq_paged_attn", "hyq_evict"):
+            getattr(L, f).restype = ctypes.c_int
         for f in ("hyq_sizes_for", "hyq_select_vertical", "hyq_quantize", "hyq_attn_prefill",
                   "hyq_prefill", "hyq_dcache_init", "hyq_freeze", "hyq_decode_append", "hyq_decode_attn",
                   "hyq_decode_attn_noalloc"):
@@ -486,3 +524,234 @@ def hyq_decode_attn_noalloc(cache: DecodeCache, q, out, softmax_scale: float | N
     o = _ptr(out, "out", nb, odt, cache.device)
     _check(lib().hyq_decode_attn_noalloc(ctypes.byref(cache.c), qp, scale, o, out_dtype,
                                          _stream(stream)))
+
+
+# --------------------------------------------------------------------------
+# paged serving: norms and rotation, the paged cache, its attention, eviction
+# --------------------------------------------------------------------------
+
+def _on_device(device, stream):
+    """The stream of a call on ``device`` (which need not be the current one)
+    and the context to make the call in."""
+    torch = _torch()
+    if device.type != "cuda":
+        raise ValueError("tensors must be on a GPU")
+    if stream is not None:
+        if getattr(stream, "device", device) != device:
+            raise ValueError(f"the stream is on {stream.device}, the tensors are on {device}")
+    else:
+        stream = torch._C._cuda_getCurrentRawStream(device.index)
+    return _stream(stream), torch.cuda.device(device)
+
+
+def _call(device, stream, fn, *args):
+    """fn(*args, stream) with ``device`` current."""
+    torch = _torch()
+    st, guard = _on_device(device, stream)
+    if torch.cuda.current_device() == device.index:
+        _check(fn(*args, st))
+    else:
+        with guard:
+            _check(fn(*args, st))
+
+
+class Rope:
+    """Norm weights and rotation of ``hyq_norm_rope`` / ``hyq_paged_append``
+    (mirrors ``hyq_rope``): ``q_weight`` and ``k_weight`` bf16 [D] or None (no
+    norm), ``inv_freq`` float32 [rot_dim / 2], radians per position."""
+
+    def __init__(self, rot_dim: int = 128, interleaved: bool = False, eps: float = 1e-6,
+                 q_weight=None, k_weight=None, inv_freq=None):
+        torch = _torch()
+        given = [t for t in (q_weight, k_weight, inv_freq) if t is not None]
+        self.device = given[0].device if given else None
+        bf, f32 = (torch.bfloat16,), (torch.float32,)
+        n = max(int(rot_dim), 0) // 2
+        self.c = _Rope(int(rot_dim), int(bool(interleaved)), float(eps),
+                       _ptr(q_weight, "q_weight", 256, bf, self.device, allow_none=True),
+                       _ptr(k_weight, "k_weight", 256, bf, self.device, allow_none=True),
+                       _ptr(inv_freq, "inv_freq", 4 * n, f32, self.device, allow_none=n == 0))
+        self.tensors = (q_weight, k_weight, inv_freq)   # keeps their memory alive
+
+
+def _row_args(t, name, T, heads, D, device):
+    """(pointer, elements from token to token) of rows [T, heads, D]."""
+    if t is None:
+        return None, 0
+    if tuple(t.shape) != (T, heads, D):
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {(T, heads, D)}")
+    if t.dtype != _torch().bfloat16:
+        raise TypeError(f"{name}: dtype {t.dtype}, expected bfloat16")
+    if t.device != device:
+        raise ValueError(f"{name} is on {t.device}, expected {device}")
+    if t.numel() == 0:
+        return None, heads * D
+    if t.stride(2) != 1 or (heads > 1 and t.stride(1) != D):
+        raise ValueError(f"{name}: the heads of a token must be contiguous")
+    stride = t.stride(0) if T > 1 else heads * D
+    return t.data_ptr(), stride
+
+
+def _rope_for(rope: Rope, device):
+    if rope.device is not None and rope.device != device:
+        raise ValueError(f"rope's tensors are on {rope.device}, expected {device}")
+    return ctypes.byref(rope.c)
+
+
+def hyq_norm_rope(shape: Shape, rope: Rope, q, k, v, pos, Q, K, V, stream=None):
+    """Norms of q and k and the rotation (see include/hyq.h): rows q [B*L, Hq,
+    D], k and v [B*L, Hkv, D] (any token stride) into Q [B, Hq, L, D], K and V
+    [B, Hkv, L, D] (or [B, H, D] with L = 1); k with K and v with V may be
+    None."""
+    torch = _torch()
+    B, Hq, Hkv, L, D = shape.B, shape.Hq, shape.Hkv, shape.L, shape.D
+    dev, T = q.device, B * L
+    a = [*_row_args(q, "q", T, Hq, D, dev), *_row_args(k, "k", T, Hkv, D, dev),
+         *_row_args(v, "v", T, Hkv, D, dev)]
+    bf = (torch.bfloat16,)
+    o = [_ptr(pos, "pos", T * 4, (torch.int32,), dev),
+         _ptr(Q, "Q", T * Hq * D * 2, bf, dev),
+         _ptr(K, "K", T * Hkv * D * 2, bf, dev, allow_none=k is None),
+         _ptr(V, "V", T * Hkv * D * 2, bf, dev, allow_none=v is None)]
+    _call(dev, stream, lib().hyq_norm_rope, ctypes.byref(_derived(shape)[0]), _rope_for(rope, dev),
+          *a, *o)
+
+
+def hyq_pcache_init(Hq: int, Hkv: int, page: int, n_pages: int, bits_kv: int = 16,
+                    kv_format: int = FMT_INT, D: int = 128):
+    """Geometry of a paged cache: (ctypes hyq_pcache with NULL buffers, dict of
+    buffer sizes)."""
+    c, z = _PCache(), _PCacheSizes()
+    _check(lib().hyq_pcache_init(Hq, Hkv, D, page, n_pages, bits_kv, kv_format, ctypes.byref(c),
+                                 ctypes.byref(z)))
+    return c, {n: getattr(z, n) for n, _ in _PCacheSizes._fields_}
+
+
+class PagedCache:
+    """A pool of pages on one device: the ``hyq_pcache`` struct and the tensors
+    that own its buffers: ``k`` and ``v`` [n_pages, Hkv, page, D] (bf16, or
+    uint8 codes), with 8 bits ``k_scale`` and ``v_scale`` [n_pages, Hkv, page],
+    and with ``mass`` the float32 weights of the same shape.  ``bufs`` gives
+    existing tensors instead (``mass`` None: not collected)."""
+
+    def __init__(self, Hq: int, Hkv: int, page: int, n_pages: int, device, bits_kv: int = 16,
+                 kv_format: int = FMT_INT, mass: bool = False, bufs: dict | None = None,
+                 D: int = 128):
+        torch = _torch()
+        self.c, self.sizes = hyq_pcache_init(Hq, Hkv, page, n_pages, bits_kv, kv_format, D)
+        dev = torch.device(device)
+        if dev.type == "cuda" and dev.index is None:
+            dev = torch.device("cuda", torch.cuda.current_device())
+        self.device = dev
+        rows, kv = (n_pages, Hkv, page), torch.bfloat16 if bits_kv == 16 else torch.uint8
+        if bufs is None:
+            def zeros(shape, dtype):
+                return torch.zeros(shape, dtype=dtype, device=dev)
+            bufs = {"k": zeros(rows + (D,), kv), "v": zeros(rows + (D,), kv)}
+            if bits_kv == 8:
+                bufs["k_scale"], bufs["v_scale"] = zeros(rows, torch.float32), zeros(rows, torch.float32)
+            if mass:
+                bufs["mass"] = zeros(rows, torch.float32)
+        self.bufs = {n: bufs.get(n) for n in _PCACHE_PTRS}
+        codes = (kv,) if bits_kv == 16 else (torch.uint8, torch.int8)
+        z, f32 = self.sizes, (torch.float32,)
+        for n, need, dtypes in (("k", z["kv_bytes"], codes), ("v", z["kv_bytes"], codes),
+                                ("k_scale", z["scale_bytes"], f32),
+                                ("v_scale", z["scale_bytes"], f32), ("mass", z["mass_bytes"], f32)):
+            setattr(self.c, n, _ptr(self.bufs[n], n, need, dtypes, dev, allow_none=n == "mass"))
+
+
+class PagedBatch:
+    """The ragged batch of one step (mirrors ``hyq_pbatch``): int32 tensors
+    ``cu_new`` [B + 1], ``lens`` [B], ``table`` [B, max_pages] and the bounds
+    ``max_new`` (new tokens of a sequence) and ``max_len`` (cached slots)."""
+
+    def __init__(self, cu_new, lens, table, max_new: int, max_len: int):
+        self.B = lens.numel()
+        if table.dim() != 2 or table.shape[0] != self.B:
+            raise ValueError(f"table has shape {tuple(table.shape)}, expected ({self.B}, pages)")
+        i32 = (_torch().int32,)
+        self.device = lens.device
+        self.c = _PBatch(self.B, 0, int(max_new), int(max_len), table.shape[1],
+                         _ptr(cu_new, "cu_new", 4 * (self.B + 1), i32, self.device),
+                         _ptr(lens, "lens", 4 * self.B, i32, self.device),
+                         _ptr(table, "table", 4 * self.B * table.shape[1], i32, self.device))
+        self.tensors = (cu_new, lens, table)   # keeps their memory alive
+
+    def of(self, T: int):
+        """The struct for a call of T token rows."""
+        return _PBatch(self.B, T, self.c.max_new, self.c.max_len, self.c.max_pages, self.c.cu_new,
+                       self.c.lens, self.c.table)
+
+
+def _batch_for(cache: PagedCache, batch: PagedBatch, T: int):
+    if batch.device != cache.device:
+        raise ValueError(f"the batch is on {batch.device}, the cache on {cache.device}")
+    return ctypes.byref(batch.of(T))
+
+
+def hyq_paged_append(cache: PagedCache, batch: PagedBatch, rope: Rope, q, k, v, pos, q_out,
+                     stream=None):
+    """hyq_norm_rope for the new tokens of a batch (rows q [T, Hq, D], k and v
+    [T, Hkv, D], pos int32 [T]): q to q_out [T, Hq, D], k and v into their
+    pages.  q and q_out may be None."""
+    torch = _torch()
+    c, dev, T = cache.c, cache.device, k.shape[0]
+    a = [*_row_args(q, "q", T, c.Hq, c.D, dev), *_row_args(k, "k", T, c.Hkv, c.D, dev),
+         *_row_args(v, "v", T, c.Hkv, c.D, dev),
+         _ptr(pos, "pos", T * 4, (torch.int32,), dev),
+         _ptr(q_out, "q_out", T * c.Hq * c.D * 2, (torch.bfloat16,), dev, allow_none=q is None)]
+    _call(dev, stream, lib().hyq_paged_append, ctypes.byref(c), _batch_for(cache, batch, T),
+          _rope_for(rope, dev), *a)
+
+
+def hyq_paged_ws_bytes(cache: PagedCache, batch: PagedBatch, mass: bool = False,
+                       T: int | None = None) -> int:
+    """Workspace bytes of hyq_paged_attn within the batch's bounds, for T token
+    rows (default: B * max_new, the most there can be)."""
+    n = ctypes.c_size_t()
+    b = batch.of(batch.B * batch.c.max_new if T is None else T)
+    _check(lib().hyq_paged_ws_bytes(ctypes.byref(cache.c), ctypes.byref(b),
+                                    MASS_SET if mass else MASS_NONE, ctypes.byref(n)))
+    return n.value
+
+
+def hyq_paged_attn(cache: PagedCache, batch: PagedBatch, q, out, softmax_scale: float | None = None,
+                   out_dtype: int = 0, mass: int = MASS_NONE, ws=None, stream=None):
+    """Causal attention of the new tokens' queries q (bf16 [T, Hq, D]) over the
+    pages of their sequences into out [T, Hq, D] (see include/hyq.h); ``mass``
+    adds the weights to the cache's mass, or sets it to them."""
+    torch = _torch()
+    c, dev, T = cache.c, cache.device, q.shape[0]
+    want = (T, c.Hq, c.D)
+    if tuple(q.shape) != want or tuple(out.shape) != want:
+        raise ValueError(f"q and out have shapes {tuple(q.shape)} and {tuple(out.shape)}, "
+                         f"expected {want}")
+    n = T * c.Hq * c.D
+    qp = _ptr(q, "q", n * 2, (torch.bfloat16,), dev)
+    o = _ptr(out, "out", n * (4 if out_dtype == 0 else 2),
+             (torch.float32,) if out_dtype == 0 else (torch.bfloat16,), dev)
+    w = _ptr(ws, "ws", 0, (torch.uint8, torch.int8, torch.float32), dev, allow_none=True)
+    wsb = 0 if ws is None else ws.numel() * ws.element_size()
+    scale = 1.0 / math.sqrt(c.D) if softmax_scale is None else softmax_scale
+    _call(dev, stream, lib().hyq_paged_attn, ctypes.byref(c), _batch_for(cache, batch, T), qp,
+          scale, int(mass), o, out_dtype, w, wsb)
+
+
+def hyq_evict(cache: PagedCache, lens, table, new_table, keep, new_lens, max_len: int, budget: int,
+              recent: int = 0, stream=None):
+    """Eviction by the cache's mass (see include/hyq.h): every KV head of the
+    sequences of ``table`` keeps ``budget`` slots, which go to the pages of
+    ``new_table``; ``keep`` [B, Hkv, budget] and ``new_lens`` [B] (int32) say
+    which and how many."""
+    i32 = (_torch().int32,)
+    c, dev, B = cache.c, cache.device, lens.numel()
+    for n, t in (("table", table), ("new_table", new_table)):
+        if t.dim() != 2 or t.shape[0] != B:
+            raise ValueError(f"{n} has shape {tuple(t.shape)}, expected ({B}, pages)")
+    a = [_ptr(lens, "lens", 4 * B, i32, dev), _ptr(table, "table", 4 * table.numel(), i32, dev)]
+    o = [_ptr(new_table, "new_table", 4 * new_table.numel(), i32, dev), new_table.shape[1],
+         _ptr(keep, "keep", 4 * B * c.Hkv * max(int(budget), 0), i32, dev),
+         _ptr(new_lens, "new_lens", 4 * B, i32, dev)]
+    _call(dev, stream, lib().hyq_evict, ctypes.byref(c), B, *a, table.shape[1], int(max_len),
+          int(budget), int(recent), *o)

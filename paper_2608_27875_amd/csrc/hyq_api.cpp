@@ -244,6 +244,99 @@ int check_decode_attn(const hyq_dcache* cache, const void* q, float softmax_scal
   return HYQ_OK;
 }
 
+// ---- paged serving ---------------------------------------------------------
+
+bool aligned16(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
+
+int check_rope(const hyq_rope* r) {
+  if (!r) return fail(HYQ_EINVAL, "rope is NULL");
+  if (r->rot_dim < 0 || r->rot_dim > hyq::kHeadDim || r->rot_dim % 16)
+    return fail(HYQ_EINVAL, "rot_dim must be a multiple of 16 in [0, %d] (got %d)", hyq::kHeadDim,
+                r->rot_dim);
+  if (r->interleaved != 0 && r->interleaved != 1)
+    return fail(HYQ_EINVAL, "interleaved must be 0 or 1 (got %d)", r->interleaved);
+  if (!(r->eps >= 0.0f) || r->eps == INFINITY)
+    return fail(HYQ_EINVAL, "eps must be finite and >= 0");
+  if (r->rot_dim > 0 && !r->inv_freq)
+    return fail(HYQ_EINVAL, "inv_freq must be non-NULL when rot_dim > 0");
+  if (!aligned16(r->q_weight) || !aligned16(r->k_weight))
+    return fail(HYQ_EINVAL, "q_weight and k_weight must be aligned to 16 bytes");
+  return HYQ_OK;
+}
+
+// One of the rows q, k, v of a norm_rope / append call.
+int check_rows(const char* name, const void* p, int64_t stride, int heads, int D) {
+  if (!p) return HYQ_OK;
+  if (stride < (int64_t)heads * D || stride % 8)
+    return fail(HYQ_EINVAL, "%s_stride must be a multiple of 8 and at least heads * D (got %lld)",
+                name, (long long)stride);
+  if (!aligned16(p)) return fail(HYQ_EINVAL, "%s must be aligned to 16 bytes", name);
+  return HYQ_OK;
+}
+
+// Geometry of a paged cache, without its buffers.
+int check_pcache_geometry(const hyq_pcache* c) {
+  if (!c) return fail(HYQ_EINVAL, "cache is NULL");
+  if (c->Hq < 1 || c->Hkv < 1 || c->D < 1 || c->n_pages < 1)
+    return fail(HYQ_EINVAL, "Hq, Hkv, D, n_pages must be >= 1 (got %d, %d, %d, %d)", c->Hq, c->Hkv,
+                c->D, c->n_pages);
+  if (c->Hq % c->Hkv) return fail(HYQ_EINVAL, "Hq (%d) must be a multiple of Hkv (%d)", c->Hq, c->Hkv);
+  if (c->page < 16 || c->page > 256 || (c->page & (c->page - 1)))
+    return fail(HYQ_EINVAL, "page must be 16, 32, 64, 128 or 256 (got %d)", c->page);
+  if (c->bits_kv != 16 && c->bits_kv != 8)
+    return fail(HYQ_EUNSUPPORTED, "pages hold 16 or 8 bits (got %d)", c->bits_kv);
+  if (c->bits_kv == 8 && c->kv_format != HYQ_FMT_INT && c->kv_format != HYQ_FMT_FP8)
+    return fail(HYQ_EUNSUPPORTED, "8-bit pages hold HYQ_FMT_INT or HYQ_FMT_FP8 codes (got %d)",
+                c->kv_format);
+  if (c->D != hyq::kHeadDim)
+    return fail(HYQ_EUNSUPPORTED, "head dim %d not supported (only %d)", c->D, hyq::kHeadDim);
+  if (c->Hq / c->Hkv > 8)
+    return fail(HYQ_EUNSUPPORTED, "GQA group size %d not supported (at most 8)", c->Hq / c->Hkv);
+  return HYQ_OK;
+}
+
+int check_pcache(const hyq_pcache* c) {
+  const int rc = check_pcache_geometry(c);
+  if (rc) return rc;
+  if (!c->k || !c->v) return fail(HYQ_EINVAL, "the cache's k and v must be non-NULL");
+  if (c->bits_kv == 8 && (!c->k_scale || !c->v_scale))
+    return fail(HYQ_EINVAL, "the cache's k_scale and v_scale must be non-NULL with 8 bits");
+  if (!aligned16(c->k) || !aligned16(c->v) || !aligned16(c->k_scale) || !aligned16(c->v_scale) ||
+      !aligned16(c->mass))
+    return fail(HYQ_EINVAL, "the cache's buffers must be aligned to 16 bytes");
+  return HYQ_OK;
+}
+
+// Bounds of a batch (its device arrays are checked by the calls that read them).
+constexpr int64_t kMaxSlots = (int64_t)1 << 23;   // of one sequence
+constexpr int64_t kMaxRows = (int64_t)1 << 24;    // query rows (tokens * heads) of one step
+int check_pbatch(const hyq_pcache* c, const hyq_pbatch* b) {
+  if (!b) return fail(HYQ_EINVAL, "batch is NULL");
+  if (b->B < 1 || b->T < 0 || b->max_new < 0 || b->max_len < 0 || b->max_pages < 1)
+    return fail(HYQ_EINVAL, "B and max_pages must be >= 1, T, max_new and max_len >= 0 (got %d, %d, "
+                "%d, %d, %d)", b->B, b->max_pages, b->T, b->max_new, b->max_len);
+  if ((int64_t)b->max_len + b->max_new > kMaxSlots)
+    return fail(HYQ_EUNSUPPORTED, "sequences of up to %lld slots not supported (at most %lld)",
+                (long long)b->max_len + b->max_new, (long long)kMaxSlots);
+  if ((int64_t)b->T * (c->Hq + 2 * c->Hkv) > kMaxRows)
+    return fail(HYQ_EUNSUPPORTED, "%d token rows in one step not supported", b->T);
+  if ((int64_t)b->B * c->Hkv > 32768)
+    return fail(HYQ_EUNSUPPORTED, "%d sequences in one step not supported", b->B);
+  return HYQ_OK;
+}
+
+int check_pbatch_arrays(const hyq_pbatch* b) {
+  if (!b->cu_new || !b->lens || !b->table)
+    return fail(HYQ_EINVAL, "the batch's cu_new, lens and table must be non-NULL");
+  return HYQ_OK;
+}
+
+int check_mass(int32_t mass) {
+  if (mass != HYQ_MASS_NONE && mass != HYQ_MASS_ADD && mass != HYQ_MASS_SET)
+    return fail(HYQ_EINVAL, "mass must be HYQ_MASS_NONE, HYQ_MASS_ADD or HYQ_MASS_SET (got %d)", mass);
+  return HYQ_OK;
+}
+
 int hip_status(hipError_t e, const char* what) {
   if (e != hipSuccess) return fail(HYQ_EHIP, "%s: %s", what, hipGetErrorString(e));
   return ok();
@@ -532,6 +625,147 @@ HYQ_API int hyq_decode_attn_noalloc(const hyq_dcache* cache, const void* q, floa
   return hip_status(hyq::launch_decode_attn(*cache, static_cast<const uint16_t*>(q), softmax_scale,
                                             out, out_dtype, part, static_cast<hipStream_t>(stream)),
                     "hyq_decode_attn_noalloc launch");
+}
+
+HYQ_API int hyq_norm_rope(const hyq_shape* shape, const hyq_rope* rope, const void* q,
+                          int64_t q_stride, const void* k, int64_t k_stride, const void* v,
+                          int64_t v_stride, const int32_t* pos, void* Q, void* K, void* V,
+                          void* stream) {
+  hyq_sizes z;
+  int rc = check_shape(shape, &z);
+  if (rc) return rc;
+  if ((rc = check_rope(rope))) return rc;
+  if (!q || !Q || !pos) return fail(HYQ_EINVAL, "q, Q and pos must be non-NULL");
+  if (!k != !K || !v != !V) return fail(HYQ_EINVAL, "k and K, v and V must be given together");
+  if ((rc = check_rows("q", q, q_stride, shape->Hq, shape->D)) ||
+      (rc = check_rows("k", k, k_stride, shape->Hkv, shape->D)) ||
+      (rc = check_rows("v", v, v_stride, shape->Hkv, shape->D)))
+    return rc;
+  if (!aligned16(Q) || !aligned16(K) || !aligned16(V))
+    return fail(HYQ_EINVAL, "Q, K and V must be aligned to 16 bytes");
+  if ((int64_t)shape->B * shape->L * (shape->Hq + 2 * shape->Hkv) > kMaxRows)
+    return fail(HYQ_EUNSUPPORTED, "%lld token rows in one call not supported",
+                (long long)shape->B * shape->L);
+  const hyq::RopeRows x = {static_cast<const uint16_t*>(q), static_cast<const uint16_t*>(k),
+                           static_cast<const uint16_t*>(v), q_stride, k_stride, v_stride, pos};
+  return hip_status(hyq::launch_norm_rope(*shape, *rope, x, static_cast<uint16_t*>(Q),
+                                          static_cast<uint16_t*>(K), static_cast<uint16_t*>(V),
+                                          static_cast<hipStream_t>(stream)),
+                    "hyq_norm_rope launch");
+}
+
+HYQ_API int hyq_pcache_init(int32_t Hq, int32_t Hkv, int32_t D, int32_t page, int32_t n_pages,
+                            int32_t bits_kv, int32_t kv_format, hyq_pcache* cache,
+                            hyq_pcache_sizes* sizes) {
+  if (!cache) return fail(HYQ_EINVAL, "cache is NULL");
+  hyq_pcache c;
+  memset(&c, 0, sizeof c);
+  c.Hq = Hq;
+  c.Hkv = Hkv;
+  c.D = D;
+  c.page = page;
+  c.n_pages = n_pages;
+  c.bits_kv = bits_kv;
+  c.kv_format = kv_format;
+  const int rc = check_pcache_geometry(&c);
+  if (rc) return rc;
+  *cache = c;
+  if (sizes) {
+    const size_t rows = (size_t)n_pages * Hkv * page;
+    sizes->kv_bytes = rows * D * (bits_kv / 8);
+    sizes->scale_bytes = bits_kv == 8 ? rows * 4 : 0;
+    sizes->mass_bytes = rows * 4;
+  }
+  return ok();
+}
+
+HYQ_API int hyq_paged_append(const hyq_pcache* cache, const hyq_pbatch* batch,
+                             const hyq_rope* rope, const void* q, int64_t q_stride, const void* k,
+                             int64_t k_stride, const void* v, int64_t v_stride,
+                             const int32_t* pos, void* q_out, void* stream) {
+  int rc = check_pcache(cache);
+  if (rc) return rc;
+  if ((rc = check_pbatch(cache, batch)) || (rc = check_rope(rope))) return rc;
+  if (batch->T == 0 || batch->max_new == 0) return ok();
+  if ((rc = check_pbatch_arrays(batch))) return rc;
+  if (!k || !v || !pos) return fail(HYQ_EINVAL, "k, v and pos must be non-NULL");
+  if (!q != !q_out) return fail(HYQ_EINVAL, "q and q_out must be given together");
+  if ((rc = check_rows("q", q, q_stride, cache->Hq, cache->D)) ||
+      (rc = check_rows("k", k, k_stride, cache->Hkv, cache->D)) ||
+      (rc = check_rows("v", v, v_stride, cache->Hkv, cache->D)))
+    return rc;
+  if (!aligned16(q_out)) return fail(HYQ_EINVAL, "q_out must be aligned to 16 bytes");
+  const hyq::RopeRows x = {static_cast<const uint16_t*>(q), static_cast<const uint16_t*>(k),
+                           static_cast<const uint16_t*>(v), q_stride, k_stride, v_stride, pos};
+  return hip_status(hyq::launch_paged_append(*cache, *batch, *rope, x, static_cast<uint16_t*>(q_out),
+                                             static_cast<hipStream_t>(stream)),
+                    "hyq_paged_append launch");
+}
+
+HYQ_API int hyq_paged_ws_bytes(const hyq_pcache* cache, const hyq_pbatch* batch, int32_t mass,
+                               size_t* bytes) {
+  if (!bytes) return fail(HYQ_EINVAL, "bytes output is NULL");
+  int rc = check_pcache_geometry(cache);
+  if (rc) return rc;
+  if ((rc = check_pbatch(cache, batch)) || (rc = check_mass(mass))) return rc;
+  *bytes = batch->T == 0 || batch->max_new == 0 ? 0 : hyq::paged_ws_bytes(*cache, *batch, mass);
+  return ok();
+}
+
+HYQ_API int hyq_paged_attn(const hyq_pcache* cache, const hyq_pbatch* batch, const void* q,
+                           float softmax_scale, int32_t mass, void* out, int32_t out_dtype,
+                           void* ws, size_t ws_bytes, void* stream) {
+  int rc = check_pcache(cache);
+  if (rc) return rc;
+  if ((rc = check_pbatch(cache, batch)) || (rc = check_mass(mass))) return rc;
+  if (mass != HYQ_MASS_NONE && !cache->mass)
+    return fail(HYQ_EINVAL, "the cache has no mass buffer to collect the weights in");
+  if (out_dtype != 0 && out_dtype != 1)
+    return fail(HYQ_EINVAL, "out_dtype must be 0 (float32) or 1 (bf16), got %d", out_dtype);
+  if (!(softmax_scale > 0.0f) || softmax_scale == INFINITY)
+    return fail(HYQ_EINVAL, "softmax_scale must be positive and finite");
+  if (batch->T == 0 || batch->max_new == 0) return ok();
+  if ((rc = check_pbatch_arrays(batch))) return rc;
+  if (!q || !out) return fail(HYQ_EINVAL, "q and out must be non-NULL");
+  if (!aligned16(q) || !aligned16(out)) return fail(HYQ_EINVAL, "q and out must be aligned to 16 bytes");
+  const size_t need = hyq::paged_ws_bytes(*cache, *batch, mass);
+  if (need > 0 && (!ws || ws_bytes < need))
+    return fail(HYQ_EINVAL, "workspace too small: %zu bytes given, %zu needed", ws_bytes, need);
+  if (!aligned16(ws)) return fail(HYQ_EINVAL, "the workspace must be aligned to 16 bytes");
+  return hip_status(hyq::launch_paged_attn(*cache, *batch, static_cast<const uint16_t*>(q),
+                                           softmax_scale, mass, out, out_dtype, ws,
+                                           static_cast<hipStream_t>(stream)),
+                    "hyq_paged_attn launch");
+}
+
+HYQ_API int hyq_evict(const hyq_pcache* cache, int32_t B, const int32_t* lens,
+                      const int32_t* table, int32_t max_pages, int32_t max_len, int32_t budget,
+                      int32_t recent, const int32_t* new_table, int32_t new_pages, int32_t* keep,
+                      int32_t* new_lens, void* stream) {
+  int rc = check_pcache(cache);
+  if (rc) return rc;
+  if (!cache->mass) return fail(HYQ_EINVAL, "eviction needs the cache's mass buffer");
+  if (B < 1 || max_pages < 1 || max_len < 0 || new_pages < 1)
+    return fail(HYQ_EINVAL, "B, max_pages and new_pages must be >= 1, max_len >= 0 (got %d, %d, %d, "
+                "%d)", B, max_pages, new_pages, max_len);
+  if (budget < 1 || recent < 0 || recent > budget)
+    return fail(HYQ_EINVAL, "budget must be >= 1 and 0 <= recent <= budget (got %d, %d)", budget, recent);
+  if ((int64_t)new_pages * cache->page < budget)
+    return fail(HYQ_EINVAL, "%d new pages of %d slots do not hold a budget of %d", new_pages,
+                cache->page, budget);
+  if (max_len > kMaxSlots)
+    return fail(HYQ_EUNSUPPORTED, "sequences of up to %d slots not supported (at most %lld)", max_len,
+                (long long)kMaxSlots);
+  if ((int64_t)B * cache->Hkv > 32768)
+    return fail(HYQ_EUNSUPPORTED, "%d sequences in one call not supported", B);
+  if (!lens || !table || !new_table || !keep || !new_lens)
+    return fail(HYQ_EINVAL, "lens, table, new_table, keep and new_lens must be non-NULL");
+  if (overlaps(lens, (size_t)B * 4, new_lens, (size_t)B * 4))
+    return fail(HYQ_EINVAL, "new_lens must not overlap lens (every KV head reads it)");
+  return hip_status(hyq::launch_evict(*cache, B, lens, table, max_pages, max_len, budget, recent,
+                                      new_table, new_pages, keep, new_lens,
+                                      static_cast<hipStream_t>(stream)),
+                    "hyq_evict launch");
 }
 
 }  // extern "C"

@@ -91,6 +91,25 @@ hipError_t launch_decode_append(const hyq_dcache& c, const uint16_t* k_new, cons
 hipError_t launch_decode_attn(const hyq_dcache& c, const uint16_t* q, float softmax_scale,
                               void* out, int out_dtype, float* part, hipStream_t st);
 
+// Paged serving.  The rows of a norm_rope / paged_append call.
+struct RopeRows {
+  const uint16_t *q, *k, *v;
+  int64_t q_stride, k_stride, v_stride;   // elements from token to token
+  const int32_t* pos;
+};
+hipError_t launch_norm_rope(const hyq_shape& s, const hyq_rope& r, const RopeRows& x, uint16_t* Q,
+                            uint16_t* K, uint16_t* V, hipStream_t st);
+hipError_t launch_paged_append(const hyq_pcache& c, const hyq_pbatch& b, const hyq_rope& r,
+                               const RopeRows& x, uint16_t* q_out, hipStream_t st);
+size_t paged_ws_bytes(const hyq_pcache& c, const hyq_pbatch& b, int mass);
+hipError_t launch_paged_attn(const hyq_pcache& c, const hyq_pbatch& b, const uint16_t* q,
+                             float softmax_scale, int mass, void* out, int out_dtype, void* ws,
+                             hipStream_t st);
+hipError_t launch_evict(const hyq_pcache& c, int B, const int32_t* lens, const int32_t* table,
+                        int max_pages, int max_len, int budget, int recent,
+                        const int32_t* new_table, int new_pages, int32_t* keep, int32_t* new_lens,
+                        hipStream_t st);
+
 // ---- device helpers -------------------------------------------------------
 
 __device__ __forceinline__ float bf16_bits_to_f32(uint32_t b) {

@@ -1,0 +1,870 @@
+// Causal attention of new tokens over a paged cache, and the attention weight
+// each cached key received.
+//
+//   z_n = alpha <q, K_n>, n <= lens + i;  out = sum w_n V_n / sum w_n,
+//   w_n = exp(z_n - max z);  mass_n (+)= sum over rows of w_n / sum w.
+//
+// The g query heads of a KV head and a sequence's new tokens are rows of one
+// product with that head's keys (row i * g + h), so a key is read once for all
+// of them.  Two kernels share the work by the number of rows:
+//
+//   few rows (new * g <= 16, single and drafted tokens): bound by HBM.  Every
+//   byte goes from memory straight into a matrix operand: a wave owns units of
+//   32 keys, S^T = K q^T in 16x16x32 products with the keys as rows; the
+//   accumulators are then the B operand of O^T = V^T P^T, whose A operand is
+//   eight rows of V transposed in registers (one byte permute per pair).
+//   many rows (chunks): bound by the matrix cores.  Workgroups of 128 rows
+//   stage tiles of 64 keys in LDS, V transposed on the way.
+//
+// Keys are split over workgroups where there are too few rows to fill the
+// chip; partial sums (acc, max, sum) then go through a workspace and a second
+// launch joins them, which also turns the logits into masses.
+#include "paged_dev.h"
+
+#include <algorithm>
+
+namespace hyq {
+namespace {
+
+typedef __bf16 v8bf __attribute__((ext_vector_type(8)));
+typedef __bf16 v2bf __attribute__((ext_vector_type(2)));
+typedef float v4f __attribute__((ext_vector_type(4)));
+typedef float v16f __attribute__((ext_vector_type(16)));
+typedef unsigned v4u __attribute__((ext_vector_type(4)));
+typedef unsigned v2u __attribute__((ext_vector_type(2)));
+
+constexpr int kBf16 = -1;            // page format beside HYQ_FMT_INT / HYQ_FMT_FP8 (8-bit codes)
+constexpr int kFewRows = 16;         // rows per KV head of the few-row kernel
+constexpr int kFewThreads = 256, kFewWaves = 4, kUnit = 32;
+constexpr int kRowTile = 128, kKeyTile = 64, kManyThreads = 256;
+constexpr int kPart = kHeadDim + 4;  // floats of a partial: acc[128], max, sum, padding
+constexpr float kLazy = 8.0f;        // rescale only when the maximum grows by more than 2^8
+constexpr float kFloor = -1.0e30f;   // start of a running maximum (finite: exp2 of -inf - it is 0)
+
+struct AttnArgs {
+  PagedGeom g;
+  const uint8_t *k, *v;
+  const float *ks, *vs;
+  float* mass;
+  const uint16_t* q;
+  void* out;
+  int out_bf16;
+  int mass_mode;
+  float c_log2;        // softmax_scale * log2(e)
+  int few_max;         // sequences of at most so many rows go to the few-row kernel
+  int S_few, S_many;   // splits of the keys in the two kernels
+  int join_few;        // whether the few-row kernel leaves partials
+  float* part;         // [S][T][Hq][kPart]
+  float* logit;        // few rows with mass: [B][Hkv][kFewRows][logit_stride]
+  int logit_stride;
+  float2* stat;        // many rows with mass: (max, 1 / sum) of every query row [T][Hq]
+};
+
+// Four codes (one dword) -> two pairs of bf16, exact (both formats have at
+// most 8 significant bits).
+template <int FMT>
+__device__ __forceinline__ void codes4_to_bf16(uint32_t w, uint32_t& lo, uint32_t& hi) {
+  if constexpr (FMT == HYQ_FMT_FP8) {
+    lo = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, false));
+    hi = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, true));
+  } else {
+    const uint32_t u = w ^ 0x80808080u;   // biased by 128: the unsigned byte conversions
+    float f[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) f[i] = (float)((u >> (8 * i)) & 0xffu) - 128.0f;
+    lo = __builtin_amdgcn_perm(__float_as_uint(f[1]), __float_as_uint(f[0]), 0x07060302u);
+    hi = __builtin_amdgcn_perm(__float_as_uint(f[3]), __float_as_uint(f[2]), 0x07060302u);
+  }
+}
+
+// Eight consecutive elements of a page row as bf16, from 16 bytes of bf16 or
+// 8 bytes of codes.
+template <int FMT>
+struct Eight {
+  using type = v2u;
+};
+template <>
+struct Eight<kBf16> {
+  using type = v4u;
+};
+template <int FMT>
+__device__ __forceinline__ v4u to_bf16(const typename Eight<FMT>::type& w) {
+  if constexpr (FMT == kBf16) {
+    return w;
+  } else {
+    v4u r;
+    uint32_t a, b;
+    codes4_to_bf16<FMT>(w[0], a, b);
+    r[0] = a;
+    r[1] = b;
+    codes4_to_bf16<FMT>(w[1], a, b);
+    r[2] = a;
+    r[3] = b;
+    return r;
+  }
+}
+template <int FMT>
+constexpr int row_bytes() {
+  return FMT == kBf16 ? 2 * kHeadDim : kHeadDim;
+}
+
+// Channel j of eight rows (each row's 8 channels as 4 pairs) in key order.
+__device__ __forceinline__ v4u column(const v4u (&r)[8], int j) {
+  v4u o;
+  const uint32_t sel = j & 1 ? 0x07060302u : 0x05040100u;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) o[e] = __builtin_amdgcn_perm(r[2 * e + 1][j >> 1], r[2 * e][j >> 1], sel);
+  return o;
+}
+
+// ---------------------------------------------------------------------------
+// Few rows.
+// ---------------------------------------------------------------------------
+
+// Registers of one unit of 32 keys: K rows of two 16-key tiles (four steps of
+// 32 channels each), eight V rows, and the scales of this lane's 8 keys.
+template <int FMT>
+struct Unit {
+  v4u k[2][FMT == kBf16 ? 4 : 2];
+  typename Eight<FMT>::type v[8];
+  v4f ks[2], vs[2];
+  bool gone;   // the page of this lane's 8 keys is missing
+};
+
+// Key of tile t, A-operand row m, within a unit: lane group G's accumulators
+// are then keys 8G .. 8G+7.
+__device__ __forceinline__ int unit_key(int t, int m) { return ((m >> 2) << 3) + (t << 2) + (m & 3); }
+
+// Channels of step s held by lane group G: any set as long as both operands
+// use the same; bf16 rows 32s + 8G, code rows 16 consecutive bytes per load.
+template <int FMT>
+__device__ __forceinline__ int step_channel(int s, int G) {
+  return FMT == kBf16 ? s * 32 + G * 8 : (s >> 1) * 64 + G * 16 + (s & 1) * 8;
+}
+
+// Pages of a unit's two halves of 16 keys (a page is at least 16 slots).
+struct UnitPages {
+  int p0, p1;
+};
+__device__ __forceinline__ UnitPages unit_pages(const PagedGeom& a, const int* __restrict__ row, int u) {
+  const int i0 = (u * kUnit) >> a.page_log2, i1 = (u * kUnit + 16) >> a.page_log2;
+  return UnitPages{i0 < a.max_pages ? row[i0] : -1, i1 < a.max_pages ? row[i1] : -1};
+}
+
+template <int FMT>
+__device__ __forceinline__ void load_unit(Unit<FMT>& r, const AttnArgs& a, UnitPages pg, int j, int u,
+                                          int hl, int G) {
+  const int mask = (1 << a.g.page_log2) - 1, base = u * kUnit;
+  const int np = a.g.n_pages;
+  const bool ok0 = (unsigned)pg.p0 < (unsigned)np, ok1 = (unsigned)pg.p1 < (unsigned)np;
+  const size_t r0 = ((size_t)(ok0 ? pg.p0 : 0) * a.g.Hkv + j) << a.g.page_log2;
+  const size_t r1 = ((size_t)(ok1 ? pg.p1 : 0) * a.g.Hkv + j) << a.g.page_log2;
+  const bool kh = hl >= 8, vh = G >= 2;   // K rows: keys 8 (hl / 4) ..; V rows: keys 8G ..
+  r.gone = !(vh ? ok1 : ok0);
+  const size_t krow = kh ? r1 : r0;
+#pragma unroll
+  for (int t = 0; t < 2; ++t) {
+    const uint8_t* p = a.k + (krow + ((base + unit_key(t, hl)) & mask)) * row_bytes<FMT>();
+#pragma unroll
+    for (int s = 0; s < (FMT == kBf16 ? 4 : 2); ++s)
+      r.k[t][s] = __builtin_nontemporal_load(
+          reinterpret_cast<const v4u*>(p + s * 64 + G * 16));
+  }
+  const size_t vrow = (vh ? r1 : r0) + ((base + 8 * G) & mask);
+  const uint8_t* p = a.v + vrow * row_bytes<FMT>() + hl * (row_bytes<FMT>() / 16);
+#pragma unroll
+  for (int e = 0; e < 8; ++e)
+    r.v[e] = __builtin_nontemporal_load(
+        reinterpret_cast<const typename Eight<FMT>::type*>(p + e * row_bytes<FMT>()));
+  if constexpr (FMT != kBf16) {
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      r.ks[e] = *reinterpret_cast<const v4f*>(a.ks + vrow + 4 * e);
+      r.vs[e] = *reinterpret_cast<const v4f*>(a.vs + vrow + 4 * e);
+    }
+  }
+}
+
+// Online softmax of one wave: lane (n = lane % 16, G): row n, O^T tiles j:
+// channels 8 (4G + r) + j of row n in register r.
+struct FewState {
+  v4f acc[8];
+  float m, l;   // running maximum (log2 units, the same on a row's 4 lanes); this lane's sum
+};
+
+__device__ __forceinline__ float rows_max(float x) {
+  x = fmaxf(x, __shfl_xor(x, 16, 64));
+  return fmaxf(x, __shfl_xor(x, 32, 64));
+}
+
+// last: the last key the lane's row sees.  lg: where this lane's 8 logits go,
+// or NULL.
+template <int FMT>
+__device__ __forceinline__ void few_unit(FewState& st, const Unit<FMT>& r, const v8bf (&q)[4],
+                                         float c, int base, int last, int n_kv, float* lg, int G) {
+  v4f s[2];
+#pragma unroll
+  for (int t = 0; t < 2; ++t) {
+    s[t] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      v4u ka;
+      if constexpr (FMT == kBf16) ka = r.k[t][i];
+      else ka = to_bf16<FMT>(v2u{r.k[t][i >> 1][(i & 1) * 2], r.k[t][i >> 1][(i & 1) * 2 + 1]});
+      s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8bf, ka), q[i], s[t], 0, 0, 0);
+    }
+  }
+  const int key0 = base + 8 * G;
+  // keys of a missing page, behind the sequence or the row's own token take no part
+  const int lim = r.gone ? -1 : last;
+  float y[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    float x = s[e >> 2][e & 3];
+    if constexpr (FMT != kBf16) x *= r.ks[e >> 2][e & 3];
+    y[e] = key0 + e <= lim ? x : -INFINITY;
+  }
+  if (lg) {
+    *reinterpret_cast<v4f*>(lg) = v4f{y[0], y[1], y[2], y[3]};
+    *reinterpret_cast<v4f*>(lg + 4) = v4f{y[4], y[5], y[6], y[7]};
+  }
+  float top = fmaxf(fmaxf(fmaxf(y[0], y[1]), fmaxf(y[2], y[3])), fmaxf(fmaxf(y[4], y[5]), fmaxf(y[6], y[7])));
+  top = rows_max(top) * c;
+  const float mnew = top > st.m + kLazy ? top : st.m;
+  if (__ballot(mnew != st.m)) {
+    const float f = __builtin_amdgcn_exp2f(st.m - mnew);
+#pragma unroll
+    for (int t = 0; t < 8; ++t) st.acc[t] *= f;
+    st.l *= f;
+    st.m = mnew;
+  }
+  const int there = r.gone ? 0 : n_kv - key0;   // of the lane's 8 keys, those somebody owns
+  // weights as a high + low bf16 pair (2^-17 relative): the kernel waits for
+  // memory, the second product is free
+  uint32_t hi[8], lo[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    float p = __builtin_amdgcn_exp2f(__builtin_fmaf(y[e], c, -st.m));
+    st.l += p;
+    if constexpr (FMT != kBf16) p *= e < there ? r.vs[e >> 2][e & 3] : 0.0f;
+    hi[e] = __float_as_uint(p) & 0xffff0000u;
+    lo[e] = __float_as_uint(p - __uint_as_float(hi[e]));
+  }
+  v4u ph, pl;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    ph[e] = __builtin_amdgcn_perm(hi[2 * e + 1], hi[2 * e], 0x07060302u);
+    const v2bf b = {(__bf16)__uint_as_float(lo[2 * e]), (__bf16)__uint_as_float(lo[2 * e + 1])};
+    pl[e] = __builtin_bit_cast(uint32_t, b);
+  }
+  // rows of V nobody owns are zero (they may hold NaN)
+  v4u rows[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    rows[e] = to_bf16<FMT>(r.v[e]);
+    if (e >= there) rows[e] = v4u{0u, 0u, 0u, 0u};
+  }
+#pragma unroll
+  for (int t = 0; t < 8; ++t) {
+    const v8bf va = __builtin_bit_cast(v8bf, column(rows, t));
+    st.acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va, __builtin_bit_cast(v8bf, ph), st.acc[t], 0, 0, 0);
+    st.acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va, __builtin_bit_cast(v8bf, pl), st.acc[t], 0, 0, 0);
+  }
+}
+
+__device__ __forceinline__ void store4(const AttnArgs& a, size_t row, int ch, v4f x) {
+  if (a.out_bf16) {
+    const v2bf p = {(__bf16)x[0], (__bf16)x[1]}, q = {(__bf16)x[2], (__bf16)x[3]};
+    *reinterpret_cast<v2u*>(static_cast<uint16_t*>(a.out) + row * kHeadDim + ch) =
+        v2u{__builtin_bit_cast(uint32_t, p), __builtin_bit_cast(uint32_t, q)};
+  } else {
+    *reinterpret_cast<v4f*>(static_cast<float*>(a.out) + row * kHeadDim + ch) = x;
+  }
+}
+
+// Workgroup (b, s, j) (j fastest: the heads of a sequence go to different
+// XCDs, the splits of one head to one): its 4 waves take even shares of the
+// units; their states are joined in LDS.
+template <int FMT>
+__global__ void __launch_bounds__(kFewThreads, 2)
+paged_few_kernel(AttnArgs a) {
+  __shared__ float w_acc[kFewWaves][kFewRows][kHeadDim];
+  __shared__ float w_m[kFewWaves][kFewRows], w_l[kFewWaves][kFewRows];
+  const int j = blockIdx.x % a.g.Hkv, bs = blockIdx.x / a.g.Hkv;
+  const int sp = bs % a.S_few, b = bs / a.S_few;
+  const Seq sq = seq_of(a.g, b);
+  const int rows = sq.n_new * a.g.g;
+  if (rows == 0 || rows > a.few_max) return;
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int lane = threadIdx.x & 63, hl = lane & 15, G = lane >> 4;
+  const int n = min(hl, rows - 1);   // lanes past the last row repeat it
+  const int i = n / a.g.g, h = n - i * a.g.g;
+  const size_t qrow = (size_t)(sq.t0 + i) * a.g.Hq + (size_t)j * a.g.g + h;
+  v8bf q[4];
+#pragma unroll
+  for (int s = 0; s < 4; ++s)
+    q[s] = *reinterpret_cast<const v8bf*>(a.q + qrow * kHeadDim + step_channel<FMT>(s, G));
+  const int last = min(sq.len + i, sq.n_kv - 1);
+
+  FewState st;
+#pragma unroll
+  for (int t = 0; t < 8; ++t) st.acc[t] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+  st.m = kFloor;
+  st.l = 0.0f;
+
+  const int nu = (sq.n_kv + kUnit - 1) / kUnit, nw = a.S_few * kFewWaves, gw = sp * kFewWaves + w;
+  const int first = (int)((int64_t)gw * nu / nw), end = (int)((int64_t)(gw + 1) * nu / nw);
+  const int* trow = a.g.table + (size_t)b * a.g.max_pages;
+  float* lg = a.logit ? a.logit + ((size_t)((size_t)b * a.g.Hkv + j) * kFewRows + hl) * a.logit_stride + 8 * G
+                      : nullptr;
+  if (lg && hl >= rows) lg = nullptr;
+  Unit<FMT> r0, r1;
+  auto proc = [&](const Unit<FMT>& r, int u) {
+    // keep the next unit's waits out of this one
+    __builtin_amdgcn_sched_barrier(0);
+    few_unit<FMT>(st, r, q, a.c_log2, u * kUnit, last, sq.n_kv, lg ? lg + (size_t)u * kUnit : nullptr, G);
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  int u = first;
+  if (u < end) {
+    load_unit<FMT>(r0, a, unit_pages(a.g, trow, u), j, u, hl, G);
+    UnitPages pg = unit_pages(a.g, trow, min(u + 1, end - 1));
+    for (; u + 2 < end; u += 2) {
+      load_unit<FMT>(r1, a, pg, j, u + 1, hl, G);
+      pg = unit_pages(a.g, trow, u + 2);
+      proc(r0, u);
+      load_unit<FMT>(r0, a, pg, j, u + 2, hl, G);
+      pg = unit_pages(a.g, trow, min(u + 3, end - 1));
+      proc(r1, u + 1);
+    }
+    if (u + 1 < end) {
+      load_unit<FMT>(r1, a, pg, j, u + 1, hl, G);
+      proc(r0, u);
+      proc(r1, u + 1);
+    } else {
+      proc(r0, u);
+    }
+  }
+
+  float l = st.l;
+  l += __shfl_xor(l, 16, 64);
+  l += __shfl_xor(l, 32, 64);
+  if (G == 0) {
+    w_m[w][hl] = st.m;
+    w_l[w][hl] = l;
+  }
+#pragma unroll
+  for (int r = 0; r < 4; ++r)
+#pragma unroll
+    for (int t = 0; t < 8; ++t) w_acc[w][hl][8 * (4 * G + r) + t] = st.acc[t][r];
+  __syncthreads();
+  for (int e = threadIdx.x; e < rows * (kHeadDim / 4); e += kFewThreads) {
+    const int rw = e >> 5, ch = (e & 31) * 4;
+    float M = w_m[0][rw];
+#pragma unroll
+    for (int x = 1; x < kFewWaves; ++x) M = fmaxf(M, w_m[x][rw]);
+    v4f acc = {0.0f, 0.0f, 0.0f, 0.0f};
+    float sum = 0.0f;
+#pragma unroll
+    for (int x = 0; x < kFewWaves; ++x) {
+      const float f = __builtin_amdgcn_exp2f(w_m[x][rw] - M);
+#pragma unroll
+      for (int c = 0; c < 4; ++c) acc[c] += w_acc[x][rw][ch + c] * f;
+      sum += w_l[x][rw] * f;
+    }
+    const int ii = rw / a.g.g;
+    const size_t row = (size_t)(sq.t0 + ii) * a.g.Hq + (size_t)j * a.g.g + (rw - ii * a.g.g);
+    if (a.join_few) {
+      float* dst = a.part + ((size_t)sp * a.g.T * a.g.Hq + row) * kPart;
+      *reinterpret_cast<v4f*>(dst + ch) = acc;
+      if (ch == 0) *reinterpret_cast<float2*>(dst + kHeadDim) = make_float2(M, sum);
+    } else {
+      store4(a, row, ch, acc * (sum > 0.0f ? 1.0f / sum : 0.0f));
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Many rows.
+// ---------------------------------------------------------------------------
+
+// Tile of 64 keys in LDS: K rows of 16 chunks of 16 bytes, chunk c of row r at
+// c ^ (r & 15); V transposed, channel rows of 8 chunks (8 keys each), chunk c
+// of channel d at c ^ ((d >> 1) & 7).  Both make the 16 lanes of a read phase
+// meet 16 different bank groups.
+struct ManyLds {
+  uint4 k[kKeyTile * 16];
+  uint4 v[kHeadDim * 8];
+  float ks[kKeyTile], vs[kKeyTile];
+  uint8_t gone[8];   // 8-key groups whose page is missing
+};
+
+// What one thread holds of the next tile: eight rows of eight channels.
+// Threads 0..127 carry V (key group tid % 8, channel group tid / 8), 128..255
+// K (key group (tid - 128) / 16, chunk tid % 16).
+template <int FMT>
+struct Stage {
+  typename Eight<FMT>::type x[8];
+  v4f s[2];
+  int page;
+};
+
+template <int FMT>
+__device__ __forceinline__ void stage_load(Stage<FMT>& g, const AttnArgs& a, int page, int j, int tile,
+                                           int kg, int chunk, bool is_v) {
+  const bool ok = (unsigned)page < (unsigned)a.g.n_pages;
+  g.page = ok ? page : -1;
+  const size_t row = pool_row(a.g, ok ? page : 0, j, tile * kKeyTile + kg * 8);
+  const uint8_t* p = (is_v ? a.v : a.k) + row * row_bytes<FMT>() + chunk * (row_bytes<FMT>() / 16);
+#pragma unroll
+  for (int e = 0; e < 8; ++e)
+    g.x[e] = *reinterpret_cast<const typename Eight<FMT>::type*>(p + e * row_bytes<FMT>());
+  if constexpr (FMT != kBf16) {
+    const float* sc = (is_v ? a.vs : a.ks) + row;
+    g.s[0] = *reinterpret_cast<const v4f*>(sc);
+    g.s[1] = *reinterpret_cast<const v4f*>(sc + 4);
+  }
+}
+
+template <int FMT>
+__device__ __forceinline__ void stage_store(const Stage<FMT>& g, ManyLds& m, int tile, int n_kv, int kg,
+                                            int chunk, bool is_v) {
+  v4u rows[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) rows[e] = to_bf16<FMT>(g.x[e]);
+  if (is_v) {
+    const int there = g.page < 0 ? 0 : n_kv - (tile * kKeyTile + kg * 8);
+    if (there < 8) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (e >= there) rows[e] = v4u{0u, 0u, 0u, 0u};
+    }
+#pragma unroll
+    for (int t = 0; t < 8; ++t) {
+      const int d = chunk * 8 + t;
+      reinterpret_cast<v4u*>(m.v)[d * 8 + (kg ^ ((d >> 1) & 7))] = column(rows, t);
+    }
+    if constexpr (FMT != kBf16) {
+      if (chunk == 0) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) m.vs[kg * 8 + e] = e < there ? g.s[e >> 2][e & 3] : 0.0f;
+      }
+    }
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const int r = kg * 8 + e;
+      reinterpret_cast<v4u*>(m.k)[r * 16 + (chunk ^ (r & 15))] = rows[e];
+    }
+    if (chunk == 0) {
+      m.gone[kg] = g.page < 0;
+      if constexpr (FMT != kBf16) {
+        *reinterpret_cast<v4f*>(m.ks + kg * 8) = g.s[0];
+        *reinterpret_cast<v4f*>(m.ks + kg * 8 + 4) = g.s[1];
+      }
+    }
+  }
+}
+
+// Key (within 32) of A-operand row m: bits 2 and 3 swapped, so that a lane's
+// accumulators 8a .. 8a+7 are the eight keys 16a + 8h .. of the next product's
+// B operand.
+__device__ __forceinline__ int many_key(int m) { return (m & 0x13) | ((m & 4) << 1) | ((m & 8) >> 1); }
+
+template <int FMT>
+__global__ void __launch_bounds__(kManyThreads, 2)
+paged_many_kernel(AttnArgs a, int tiles) {
+  __shared__ ManyLds lds[2];
+  const int j = blockIdx.x % a.g.Hkv;
+  int id = blockIdx.x / a.g.Hkv;
+  const int sp = id % a.S_many;
+  id /= a.S_many;
+  const int t = tiles - 1 - id % tiles, b = id / tiles;   // the longest scans first
+  const Seq sq = seq_of(a.g, b);
+  const int rows = sq.n_new * a.g.g;
+  if (rows <= a.few_max || t * kRowTile >= rows) return;
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int lane = threadIdx.x & 63, n = lane & 31, hf = lane >> 5;
+  const int r_mine = t * kRowTile + w * 32 + n;
+  const int rr = min(r_mine, rows - 1);
+  const int i = rr / a.g.g, h = rr - i * a.g.g;
+  const size_t qrow = (size_t)(sq.t0 + i) * a.g.Hq + (size_t)j * a.g.g + h;
+  v8bf q[8];
+#pragma unroll
+  for (int s = 0; s < 8; ++s)
+    q[s] = *reinterpret_cast<const v8bf*>(a.q + qrow * kHeadDim + 16 * s + 8 * hf);
+  const int last = min(sq.len + i, sq.n_kv - 1);
+  // keys any row of the workgroup sees, keys every row of it sees
+  const int i_first = (t * kRowTile) / a.g.g, i_last = (min((t + 1) * kRowTile, rows) - 1) / a.g.g;
+  const int n_keys = min(sq.len + i_last + 1, sq.n_kv), n_all = min(sq.len + i_first + 1, sq.n_kv);
+  const int nt = (n_keys + kKeyTile - 1) / kKeyTile;
+  const int first = (int)((int64_t)sp * nt / a.S_many), end = (int)((int64_t)(sp + 1) * nt / a.S_many);
+
+  v16f acc[4];
+#pragma unroll
+  for (int d = 0; d < 4; ++d)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) acc[d][e] = 0.0f;
+  float m = kFloor, l = 0.0f;
+
+  const bool is_v = threadIdx.x < 128;
+  const int st = threadIdx.x & 127;
+  const int kg = is_v ? st & 7 : st >> 4, chunk = is_v ? st >> 3 : st & 15;
+  Stage<FMT> g;
+  if (first < end) {
+    stage_load<FMT>(g, a, page_of(a.g, b, first * kKeyTile + kg * 8), j, first, kg, chunk, is_v);
+    stage_store<FMT>(g, lds[first & 1], first, sq.n_kv, kg, chunk, is_v);
+    int page = page_of(a.g, b, min(first + 1, end - 1) * kKeyTile + kg * 8);
+    for (int tile = first; tile < end; ++tile) {
+      if (tile + 1 < end) stage_load<FMT>(g, a, page, j, tile + 1, kg, chunk, is_v);
+      page = page_of(a.g, b, min(tile + 2, end - 1) * kKeyTile + kg * 8);
+      __syncthreads();
+      const ManyLds& T = lds[tile & 1];
+      v16f s[2];
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) s[x][e] = 0.0f;
+        const int r = x * 32 + many_key(n);
+#pragma unroll
+        for (int c = 0; c < 8; ++c) {
+          const v4u ka = reinterpret_cast<const v4u*>(T.k)[r * 16 + ((2 * c + hf) ^ (r & 15))];
+          s[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8bf, ka), q[c], s[x], 0, 0, 0);
+        }
+      }
+      if constexpr (FMT != kBf16) {
+#pragma unroll
+        for (int x = 0; x < 2; ++x)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) s[x][e] *= T.ks[x * 32 + (e >> 3) * 16 + hf * 8 + (e & 7)];
+      }
+      const uint64_t gone = *reinterpret_cast<const uint64_t*>(T.gone);
+      if (gone != 0 || (tile + 1) * kKeyTile > n_all) {
+#pragma unroll
+        for (int x = 0; x < 2; ++x)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            const int grp = x * 4 + (e >> 3) * 2 + hf, key = tile * kKeyTile + grp * 8 + (e & 7);
+            const bool hid = key > last || ((gone >> (8 * grp)) & 1);
+            s[x][e] = hid ? -INFINITY : s[x][e];
+          }
+      }
+      float top = s[0][0];
+#pragma unroll
+      for (int x = 0; x < 2; ++x)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) top = fmaxf(top, s[x][e]);
+      top = fmaxf(top, __shfl_xor(top, 32, 64)) * a.c_log2;
+      const float mnew = top > m + kLazy ? top : m;
+      if (__ballot(mnew != m)) {
+        const float f = __builtin_amdgcn_exp2f(m - mnew);
+#pragma unroll
+        for (int d = 0; d < 4; ++d)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) acc[d][e] *= f;
+        l *= f;
+        m = mnew;
+      }
+#pragma unroll
+      for (int x = 0; x < 2; ++x)
+#pragma unroll
+        for (int o = 0; o < 2; ++o) {
+          v8bf p;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            float pw = __builtin_amdgcn_exp2f(__builtin_fmaf(s[x][o * 8 + e], a.c_log2, -m));
+            l += pw;
+            if constexpr (FMT != kBf16) pw *= T.vs[x * 32 + o * 16 + hf * 8 + e];
+            p[e] = (__bf16)pw;
+          }
+          const int ck = x * 4 + o * 2 + hf;
+#pragma unroll
+          for (int d = 0; d < 4; ++d) {
+            const int ch = d * 32 + n;
+            const v4u va = reinterpret_cast<const v4u*>(T.v)[ch * 8 + (ck ^ ((ch >> 1) & 7))];
+            acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8bf, va), p, acc[d], 0, 0, 0);
+          }
+        }
+      if (tile + 1 < end) stage_store<FMT>(g, lds[(tile + 1) & 1], tile + 1, sq.n_kv, kg, chunk, is_v);
+    }
+  }
+  l += __shfl_xor(l, 32, 64);
+  if (r_mine >= rows) return;
+  if (a.S_many > 1) {
+    float* dst = a.part + ((size_t)sp * a.g.T * a.g.Hq + qrow) * kPart;
+#pragma unroll
+    for (int d = 0; d < 4; ++d)
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        *reinterpret_cast<v4f*>(dst + d * 32 + e * 8 + hf * 4) =
+            v4f{acc[d][4 * e], acc[d][4 * e + 1], acc[d][4 * e + 2], acc[d][4 * e + 3]};
+    if (hf == 0) *reinterpret_cast<float2*>(dst + kHeadDim) = make_float2(m, l);
+  } else {
+    const float inv = l > 0.0f ? 1.0f / l : 0.0f;
+#pragma unroll
+    for (int d = 0; d < 4; ++d)
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        store4(a, qrow, d * 32 + e * 8 + hf * 4,
+               v4f{acc[d][4 * e], acc[d][4 * e + 1], acc[d][4 * e + 2], acc[d][4 * e + 3]} * inv);
+    if (a.stat && hf == 0) a.stat[qrow] = make_float2(m, inv);
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Joining the splits.
+// ---------------------------------------------------------------------------
+
+constexpr int kJoinThreads = 128, kJoinShares = kJoinThreads / 32;
+
+// One workgroup per query row: 4 shares of the partials, 32 lanes of 4
+// channels each, joined through LDS.
+__global__ void __launch_bounds__(kJoinThreads)
+paged_join_kernel(AttnArgs a) {
+  __shared__ v4f x_acc[kJoinShares][32];
+  __shared__ float x_m[kJoinShares], x_l[kJoinShares];
+  const int t = blockIdx.x / a.g.Hq;
+  const int b = seq_of_token(a.g, t);
+  if (b < 0) return;
+  const Seq sq = seq_of(a.g, b);
+  if (t - sq.t0 >= sq.n_new) return;
+  const bool few = sq.n_new * a.g.g <= a.few_max;
+  const int S = few ? a.S_few : a.S_many;
+  if (few ? !a.join_few : S == 1) return;   // written by the attention itself
+  const size_t row = blockIdx.x;
+  const int c4 = threadIdx.x & 31, ph = threadIdx.x >> 5;
+  const float* base = a.part + row * kPart;
+  const size_t stride = (size_t)a.g.T * a.g.Hq * kPart;
+  float M = kFloor, L = 0.0f;
+  v4f acc = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 4
+  for (int s = ph; s < S; s += kJoinShares) {
+    const v4f x = *reinterpret_cast<const v4f*>(base + s * stride + c4 * 4);
+    const float2 ml = *reinterpret_cast<const float2*>(base + s * stride + kHeadDim);
+    const float mn = fmaxf(M, ml.x);
+    const float f = __builtin_amdgcn_exp2f(M - mn), e = __builtin_amdgcn_exp2f(ml.x - mn);
+    acc = acc * f + x * e;
+    L = L * f + ml.y * e;
+    M = mn;
+  }
+  x_acc[ph][c4] = acc;
+  if (c4 == 0) {
+    x_m[ph] = M;
+    x_l[ph] = L;
+  }
+  __syncthreads();
+  if (ph != 0) return;
+#pragma unroll
+  for (int s = 1; s < kJoinShares; ++s) {
+    const float mn = fmaxf(M, x_m[s]);
+    const float f = __builtin_amdgcn_exp2f(M - mn), e = __builtin_amdgcn_exp2f(x_m[s] - mn);
+    acc = acc * f + x_acc[s][c4] * e;
+    L = L * f + x_l[s] * e;
+    M = mn;
+  }
+  const float inv = L > 0.0f ? 1.0f / L : 0.0f;
+  store4(a, row, c4 * 4, acc * inv);
+  if (a.stat && c4 == 0) a.stat[row] = make_float2(M, inv);
+}
+
+// ---------------------------------------------------------------------------
+// Masses.
+// ---------------------------------------------------------------------------
+
+__device__ __forceinline__ void add_mass(const AttnArgs& a, int b, int j, int key, float x) {
+  const int p = page_of(a.g, b, key);
+  if (p < 0) return;
+  float* m = a.mass + pool_row(a.g, p, j, key);
+  *m = a.mass_mode == HYQ_MASS_ADD ? *m + x : x;
+}
+
+constexpr int kMassThreads = 256;
+
+// Few rows: from the stored logits.  Workgroup (b, j, 256 keys).
+__global__ void __launch_bounds__(kMassThreads)
+paged_few_mass_kernel(AttnArgs a) {
+  const int j = blockIdx.x % a.g.Hkv, b = blockIdx.x / a.g.Hkv;
+  const Seq sq = seq_of(a.g, b);
+  const int rows = sq.n_new * a.g.g, key = blockIdx.y * kMassThreads + threadIdx.x;
+  if (rows == 0 || rows > a.few_max || key >= sq.n_kv) return;
+  const float* lg = a.logit + ((size_t)b * a.g.Hkv + j) * kFewRows * a.logit_stride + key;
+  float sum = 0.0f;
+  for (int r = 0; r < rows; ++r) {
+    const int i = r / a.g.g;
+    const float2 ml = a.stat[(size_t)(sq.t0 + i) * a.g.Hq + (size_t)j * a.g.g + (r - i * a.g.g)];
+    sum += __builtin_amdgcn_exp2f(__builtin_fmaf(lg[(size_t)r * a.logit_stride], a.c_log2, -ml.x)) * ml.y;
+  }
+  add_mass(a, b, j, key, sum);
+}
+
+// Many rows: the products again, now that every row's maximum and sum are
+// known.  A wave owns 32 keys (its K rows stay in registers) and walks the
+// rows that see them in tiles of 32.
+template <int FMT>
+__global__ void __launch_bounds__(kMassThreads)
+paged_many_mass_kernel(AttnArgs a) {
+  const int j = blockIdx.x % a.g.Hkv, b = blockIdx.x / a.g.Hkv;
+  const Seq sq = seq_of(a.g, b);
+  const int rows = sq.n_new * a.g.g;
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int lane = threadIdx.x & 63, n = lane & 31, hf = lane >> 5;
+  const int key0 = (blockIdx.y * 4 + w) * 32;
+  if (rows <= a.few_max || key0 >= sq.n_kv) return;
+  v8bf kf[8];
+  float ks = 1.0f;
+  {
+    const int key = key0 + n, p = page_of(a.g, b, key);
+    const size_t row = pool_row(a.g, max(p, 0), j, key);
+    const uint8_t* src = a.k + row * row_bytes<FMT>();
+#pragma unroll
+    for (int c = 0; c < 8; ++c)
+      kf[c] = __builtin_bit_cast(v8bf, to_bf16<FMT>(*reinterpret_cast<const typename Eight<FMT>::type*>(
+                                           src + (2 * c + hf) * (row_bytes<FMT>() / 16))));
+    if constexpr (FMT != kBf16) ks = a.ks[row];
+  }
+  float kse[16], sum[16];
+#pragma unroll
+  for (int e = 0; e < 16; ++e) {
+    const int m = 8 * (e >> 2) + 4 * hf + (e & 3);   // accumulator row = key
+    kse[e] = __shfl(ks, m, 64);
+    sum[e] = 0.0f;
+  }
+  // rows that see the first of these keys: from token max(0, key0 - len) on
+  const int r0 = max(0, key0 - sq.len) * a.g.g / 32 * 32;
+  for (int r = r0; r < rows; r += 32) {
+    const int rr = min(r + n, rows - 1);
+    const int i = rr / a.g.g, h = rr - i * a.g.g;
+    const size_t qrow = (size_t)(sq.t0 + i) * a.g.Hq + (size_t)j * a.g.g + h;
+    v16f s;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) s[e] = 0.0f;
+#pragma unroll
+    for (int c = 0; c < 8; ++c) {
+      const v8bf q = *reinterpret_cast<const v8bf*>(a.q + qrow * kHeadDim + 16 * c + 8 * hf);
+      s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[c], q, s, 0, 0, 0);
+    }
+    float2 ml = a.stat[qrow];
+    if (r + n >= rows) ml.y = 0.0f;
+    const int last = min(sq.len + i, sq.n_kv - 1);
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      const int key = key0 + 8 * (e >> 2) + 4 * hf + (e & 3);
+      float x = s[e];
+      if constexpr (FMT != kBf16) x *= kse[e];
+      const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(x, a.c_log2, -ml.x)) * ml.y;
+      sum[e] += key <= last && ml.y > 0.0f ? p : 0.0f;
+    }
+  }
+#pragma unroll
+  for (int e = 0; e < 16; ++e) {
+    float x = sum[e];
+#pragma unroll
+    for (int o = 16; o >= 1; o >>= 1) x += __shfl_xor(x, o, 64);
+    const int key = key0 + 8 * (e >> 2) + 4 * hf + (e & 3);
+    if (n == 0 && key < sq.n_kv) add_mass(a, b, j, key, x);
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Plan.
+// ---------------------------------------------------------------------------
+
+struct Plan {
+  bool few, many;      // which kernels the batch can need
+  int few_max;
+  int S_few, S_many;
+  bool join_few, join_many;
+  int row_tiles;       // row tiles of a sequence in the many-row kernel
+  int64_t n_kv;        // bound on a sequence's slots
+  int logit_stride;
+  size_t part, logit, stat;   // workspace bytes
+  size_t total() const { return part + logit + stat; }
+};
+
+size_t up256(size_t x) { return (x + 255) & ~(size_t)255; }
+
+Plan plan_of(const hyq_pcache& c, const hyq_pbatch& b, int mass) {
+  Plan p = {};
+  const int g = c.Hq / c.Hkv;
+  const int rows = b.max_new * g;   // not of T: the workspace then grows with T
+  p.many = rows > kFewRows;
+  p.few = !p.many || b.B > 1;   // a mixed batch may hold single tokens
+  p.few_max = p.few ? kFewRows : 0;
+  p.n_kv = std::min((int64_t)b.max_len + b.max_new, (int64_t)b.max_pages * c.page);
+  const int64_t heads = (int64_t)b.B * c.Hkv;
+  const int64_t units = std::max<int64_t>(1, (p.n_kv + kUnit - 1) / kUnit);
+  const int64_t ktiles = std::max<int64_t>(1, (p.n_kv + kKeyTile - 1) / kKeyTile);
+  p.S_few = (int)std::max<int64_t>(1, std::min({(512 + heads - 1) / heads, (units + 7) / 8, (int64_t)64}));
+  p.row_tiles = (rows + kRowTile - 1) / kRowTile;
+  const int64_t wg = heads * p.row_tiles;
+  p.S_many = (int)std::max<int64_t>(1, std::min({512 / wg, (ktiles + 7) / 8, (int64_t)64}));
+  p.join_few = p.few && (p.S_few > 1 || mass);
+  p.join_many = p.many && p.S_many > 1;
+  const int S = std::max(p.join_few ? p.S_few : 0, p.join_many ? p.S_many : 0);
+  const size_t qrows = (size_t)b.T * c.Hq;
+  p.part = up256((size_t)S * qrows * kPart * 4);
+  if (mass) {
+    p.stat = up256(qrows * sizeof(float2));
+    if (p.few) {
+      p.logit_stride = (int)(units * kUnit);
+      p.logit = up256((size_t)heads * kFewRows * p.logit_stride * 4);
+    }
+  }
+  return p;
+}
+
+template <int FMT>
+hipError_t launch(const Plan& p, const AttnArgs& a, hipStream_t st) {
+  const unsigned heads = (unsigned)(a.g.B * a.g.Hkv);
+  if (p.few) paged_few_kernel<FMT><<<heads * p.S_few, kFewThreads, 0, st>>>(a);
+  if (p.many)
+    paged_many_kernel<FMT><<<heads * p.row_tiles * p.S_many, kManyThreads, 0, st>>>(a, p.row_tiles);
+  if (p.join_few || p.join_many)
+    paged_join_kernel<<<(unsigned)(a.g.T * a.g.Hq), kJoinThreads, 0, st>>>(a);
+  if (a.mass_mode != HYQ_MASS_NONE) {
+    if (p.few)
+      paged_few_mass_kernel<<<dim3(heads, (unsigned)((p.n_kv + kMassThreads - 1) / kMassThreads)),
+                              kMassThreads, 0, st>>>(a);
+    if (p.many)
+      paged_many_mass_kernel<FMT><<<dim3(heads, (unsigned)((p.n_kv + 127) / 128)), kMassThreads, 0, st>>>(a);
+  }
+  return hipGetLastError();
+}
+
+}  // namespace
+
+size_t paged_ws_bytes(const hyq_pcache& c, const hyq_pbatch& b, int mass) {
+  return plan_of(c, b, mass).total();
+}
+
+hipError_t launch_paged_attn(const hyq_pcache& c, const hyq_pbatch& b, const uint16_t* q,
+                             float softmax_scale, int mass, void* out, int out_dtype, void* ws,
+                             hipStream_t st) {
+  const Plan p = plan_of(c, b, mass);
+  AttnArgs a = {};
+  a.g = paged_geom(c, b);
+  a.k = static_cast<const uint8_t*>(c.k);
+  a.v = static_cast<const uint8_t*>(c.v);
+  a.ks = c.k_scale;
+  a.vs = c.v_scale;
+  a.mass = c.mass;
+  a.q = q;
+  a.out = out;
+  a.out_bf16 = out_dtype;
+  a.mass_mode = mass;
+  a.c_log2 = softmax_scale * 1.44269504088896340736f;
+  a.few_max = p.few_max;
+  a.S_few = p.S_few;
+  a.S_many = p.S_many;
+  a.join_few = p.join_few;
+  char* w = static_cast<char*>(ws);
+  if (p.part) a.part = reinterpret_cast<float*>(w);
+  if (p.logit) a.logit = reinterpret_cast<float*>(w + p.part);
+  a.logit_stride = p.logit_stride;
+  if (p.stat) a.stat = reinterpret_cast<float2*>(w + p.part + p.logit);
+  if (c.bits_kv == 16) return launch<kBf16>(p, a, st);
+  if (c.kv_format == HYQ_FMT_FP8) return launch<HYQ_FMT_FP8>(p, a, st);
+  return launch<HYQ_FMT_INT>(p, a, st);
+}
+
+}  // namespace hyq
