@@ -39,6 +39,7 @@ constexpr int kFewThreads = 256, kFewWaves = 4, kUnit = 32;
 constexpr int kRowTile = 128, kKeyTile = 64, kManyThreads = 256;
 constexpr int kPart = kHeadDim + 4;  // floats of a partial: acc[128], max, sum, padding
 constexpr float kLazy = 8.0f;        // rescale only when the maximum grows by more than 2^8
+constexpr float kNever = 3.0e38f;    // the "maximum" of a row that sees nothing: exp2(z - it) is 0
 constexpr float kFloor = -1.0e30f;   // start of a running maximum (finite: exp2 of -inf - it is 0)
 
 struct AttnArgs {
@@ -607,31 +608,22 @@ paged_many_kernel(AttnArgs a, int tiles) {
       for (int e = 0; e < 4; ++e)
         store4(a, qrow, d * 32 + e * 8 + hf * 4,
                v4f{acc[d][4 * e], acc[d][4 * e + 1], acc[d][4 * e + 2], acc[d][4 * e + 3]} * inv);
-    if (a.stat && hf == 0) a.stat[qrow] = make_float2(m, inv);
+    if (a.stat && hf == 0) a.stat[qrow] = make_float2(l > 0.0f ? m : kNever, inv);
   }
 }
 
 // ---------------------------------------------------------------------------
-// Joining the splits.
+// Joining the splits, and masses.
 // ---------------------------------------------------------------------------
 
 constexpr int kJoinThreads = 128, kJoinShares = kJoinThreads / 32;
+constexpr int kMassKeys = kJoinThreads * 4;   // keys of a mass workgroup of the few-row path
 
-// One workgroup per query row: 4 shares of the partials, 32 lanes of 4
-// channels each, joined through LDS.
-__global__ void __launch_bounds__(kJoinThreads)
-paged_join_kernel(AttnArgs a) {
+// Row `row` (token * Hq + head) of the output from its S partials: 4 shares of
+// them, 32 lanes of 4 channels each, joined through LDS.
+__device__ __forceinline__ void join_row(const AttnArgs& a, size_t row, int S) {
   __shared__ v4f x_acc[kJoinShares][32];
   __shared__ float x_m[kJoinShares], x_l[kJoinShares];
-  const int t = blockIdx.x / a.g.Hq;
-  const int b = seq_of_token(a.g, t);
-  if (b < 0) return;
-  const Seq sq = seq_of(a.g, b);
-  if (t - sq.t0 >= sq.n_new) return;
-  const bool few = sq.n_new * a.g.g <= a.few_max;
-  const int S = few ? a.S_few : a.S_many;
-  if (few ? !a.join_few : S == 1) return;   // written by the attention itself
-  const size_t row = blockIdx.x;
   const int c4 = threadIdx.x & 31, ph = threadIdx.x >> 5;
   const float* base = a.part + row * kPart;
   const size_t stride = (size_t)a.g.T * a.g.Hq * kPart;
@@ -664,105 +656,187 @@ paged_join_kernel(AttnArgs a) {
   }
   const float inv = L > 0.0f ? 1.0f / L : 0.0f;
   store4(a, row, c4 * 4, acc * inv);
-  if (a.stat && c4 == 0) a.stat[row] = make_float2(M, inv);
+  if (a.stat && c4 == 0) a.stat[row] = make_float2(L > 0.0f ? M : kNever, inv);
 }
 
-// ---------------------------------------------------------------------------
-// Masses.
-// ---------------------------------------------------------------------------
+// Chunks whose keys were split: one workgroup per query row of the step.
+__global__ void __launch_bounds__(kJoinThreads)
+paged_join_kernel(AttnArgs a) {
+  const int t = blockIdx.x / a.g.Hq;
+  const int b = seq_of_token(a.g, t);
+  if (b < 0) return;
+  const Seq sq = seq_of(a.g, b);
+  if (t - sq.t0 >= sq.n_new || sq.n_new * a.g.g <= a.few_max) return;
+  join_row(a, blockIdx.x, a.S_many);
+}
 
-__device__ __forceinline__ void add_mass(const AttnArgs& a, int b, int j, int key, float x) {
+// After the few-row kernel: workgroups (b, j, y) with y < kFewRows join query
+// row y; the others (with masses) take 512 keys each: the maximum and the sum
+// of every row from the partials, then the weights from the stored logits (4
+// keys a thread, rows in order).
+__global__ void __launch_bounds__(kJoinThreads)
+paged_few_finish_kernel(AttnArgs a) {
+  const int j = blockIdx.x % a.g.Hkv, b = blockIdx.x / a.g.Hkv;
+  const Seq sq = seq_of(a.g, b);
+  const int rows = sq.n_new * a.g.g;
+  if (rows == 0 || rows > a.few_max) return;
+  auto row_of = [&](int r) {
+    const int i = r / a.g.g;
+    return (size_t)(sq.t0 + i) * a.g.Hq + (size_t)j * a.g.g + (r - i * a.g.g);
+  };
+  if (blockIdx.y < kFewRows) {
+    if ((int)blockIdx.y < rows) join_row(a, row_of(blockIdx.y), a.S_few);
+    return;
+  }
+  const int key = (blockIdx.y - kFewRows) * kMassKeys + (int)threadIdx.x * 4;
+  if (key - (int)threadIdx.x * 4 >= sq.n_kv) return;
+  __shared__ float2 st[kFewRows];
+  if ((int)threadIdx.x < rows * 4) {   // 4 threads a row (at most 64: one wave)
+    const int r = threadIdx.x >> 2;
+    const float* base = a.part + row_of(r) * kPart + kHeadDim;
+    const size_t stride = (size_t)a.g.T * a.g.Hq * kPart;
+    float M = kFloor, L = 0.0f;
+    for (int s = threadIdx.x & 3; s < a.S_few; s += 4) {
+      const float2 ml = *reinterpret_cast<const float2*>(base + s * stride);
+      const float mn = fmaxf(M, ml.x);
+      L = L * __builtin_amdgcn_exp2f(M - mn) + ml.y * __builtin_amdgcn_exp2f(ml.x - mn);
+      M = mn;
+    }
+#pragma unroll
+    for (int o = 1; o < 4; o <<= 1) {
+      const float m2 = __shfl_xor(M, o, 64), l2 = __shfl_xor(L, o, 64);
+      const float mn = fmaxf(M, m2);
+      L = L * __builtin_amdgcn_exp2f(M - mn) + l2 * __builtin_amdgcn_exp2f(m2 - mn);
+      M = mn;
+    }
+    if ((threadIdx.x & 3) == 0) st[r] = make_float2(L > 0.0f ? M : kNever, L > 0.0f ? 1.0f / L : 0.0f);
+  }
+  __syncthreads();
+  if (key >= sq.n_kv) return;
+  const float* lg = a.logit + ((size_t)b * a.g.Hkv + j) * kFewRows * a.logit_stride + key;
+  v4f sum = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 4
+  for (int r = 0; r < rows; ++r) {
+    const v4f z = *reinterpret_cast<const v4f*>(lg + (size_t)r * a.logit_stride);
+    const float2 ml = st[r];
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      sum[e] = __builtin_fmaf(__builtin_amdgcn_exp2f(__builtin_fmaf(z[e], a.c_log2, -ml.x)), ml.y, sum[e]);
+  }
   const int p = page_of(a.g, b, key);
   if (p < 0) return;
   float* m = a.mass + pool_row(a.g, p, j, key);
-  *m = a.mass_mode == HYQ_MASS_ADD ? *m + x : x;
-}
-
-constexpr int kMassThreads = 256;
-
-// Few rows: from the stored logits.  Workgroup (b, j, 256 keys).
-__global__ void __launch_bounds__(kMassThreads)
-paged_few_mass_kernel(AttnArgs a) {
-  const int j = blockIdx.x % a.g.Hkv, b = blockIdx.x / a.g.Hkv;
-  const Seq sq = seq_of(a.g, b);
-  const int rows = sq.n_new * a.g.g, key = blockIdx.y * kMassThreads + threadIdx.x;
-  if (rows == 0 || rows > a.few_max || key >= sq.n_kv) return;
-  const float* lg = a.logit + ((size_t)b * a.g.Hkv + j) * kFewRows * a.logit_stride + key;
-  float sum = 0.0f;
-  for (int r = 0; r < rows; ++r) {
-    const int i = r / a.g.g;
-    const float2 ml = a.stat[(size_t)(sq.t0 + i) * a.g.Hq + (size_t)j * a.g.g + (r - i * a.g.g)];
-    sum += __builtin_amdgcn_exp2f(__builtin_fmaf(lg[(size_t)r * a.logit_stride], a.c_log2, -ml.x)) * ml.y;
+  const int n = min(4, sq.n_kv - key);
+  if (n == 4) {
+    v4f* m4 = reinterpret_cast<v4f*>(m);
+    *m4 = a.mass_mode == HYQ_MASS_ADD ? *m4 + sum : sum;
+  } else {
+    for (int e = 0; e < n; ++e) m[e] = a.mass_mode == HYQ_MASS_ADD ? m[e] + sum[e] : sum[e];
   }
-  add_mass(a, b, j, key, sum);
 }
 
 // Many rows: the products again, now that every row's maximum and sum are
-// known.  A wave owns 32 keys (its K rows stay in registers) and walks the
-// rows that see them in tiles of 32.
-template <int FMT>
-__global__ void __launch_bounds__(kMassThreads)
+// known.  A wave owns KW * 32 keys (their K rows stay in registers); the
+// workgroup walks the rows that see any of its keys in tiles of 32, staged in
+// LDS for its four waves (chunk c of row r at c ^ (r & 15)), the next tile's
+// loads in flight.
+constexpr int kMassThreads = 256;
+
+template <int FMT, int KW>
+__global__ void __launch_bounds__(kMassThreads, KW == 2 ? 2 : 3)
 paged_many_mass_kernel(AttnArgs a) {
+  __shared__ v4u qs[2][32 * 16];
+  __shared__ float2 ss[2][32];
   const int j = blockIdx.x % a.g.Hkv, b = blockIdx.x / a.g.Hkv;
   const Seq sq = seq_of(a.g, b);
   const int rows = sq.n_new * a.g.g;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int lane = threadIdx.x & 63, n = lane & 31, hf = lane >> 5;
-  const int key0 = (blockIdx.y * 4 + w) * 32;
-  if (rows <= a.few_max || key0 >= sq.n_kv) return;
-  v8bf kf[8];
-  float ks = 1.0f;
-  {
-    const int key = key0 + n, p = page_of(a.g, b, key);
+  const int wg_key = blockIdx.y * (4 * KW * 32), key0 = wg_key + w * (KW * 32);
+  if (rows <= a.few_max || wg_key >= sq.n_kv) return;
+  v8bf kf[KW][8];
+  float kse[KW][16], sum[KW][16];
+#pragma unroll
+  for (int x = 0; x < KW; ++x) {
+    const int key = key0 + x * 32 + n, p = page_of(a.g, b, key);
     const size_t row = pool_row(a.g, max(p, 0), j, key);
     const uint8_t* src = a.k + row * row_bytes<FMT>();
 #pragma unroll
     for (int c = 0; c < 8; ++c)
-      kf[c] = __builtin_bit_cast(v8bf, to_bf16<FMT>(*reinterpret_cast<const typename Eight<FMT>::type*>(
-                                           src + (2 * c + hf) * (row_bytes<FMT>() / 16))));
+      kf[x][c] = __builtin_bit_cast(v8bf, to_bf16<FMT>(*reinterpret_cast<const typename Eight<FMT>::type*>(
+                                              src + (2 * c + hf) * (row_bytes<FMT>() / 16))));
+    float ks = 1.0f;
     if constexpr (FMT != kBf16) ks = a.ks[row];
-  }
-  float kse[16], sum[16];
-#pragma unroll
-  for (int e = 0; e < 16; ++e) {
-    const int m = 8 * (e >> 2) + 4 * hf + (e & 3);   // accumulator row = key
-    kse[e] = __shfl(ks, m, 64);
-    sum[e] = 0.0f;
-  }
-  // rows that see the first of these keys: from token max(0, key0 - len) on
-  const int r0 = max(0, key0 - sq.len) * a.g.g / 32 * 32;
-  for (int r = r0; r < rows; r += 32) {
-    const int rr = min(r + n, rows - 1);
-    const int i = rr / a.g.g, h = rr - i * a.g.g;
-    const size_t qrow = (size_t)(sq.t0 + i) * a.g.Hq + (size_t)j * a.g.g + h;
-    v16f s;
-#pragma unroll
-    for (int e = 0; e < 16; ++e) s[e] = 0.0f;
-#pragma unroll
-    for (int c = 0; c < 8; ++c) {
-      const v8bf q = *reinterpret_cast<const v8bf*>(a.q + qrow * kHeadDim + 16 * c + 8 * hf);
-      s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[c], q, s, 0, 0, 0);
-    }
-    float2 ml = a.stat[qrow];
-    if (r + n >= rows) ml.y = 0.0f;
-    const int last = min(sq.len + i, sq.n_kv - 1);
 #pragma unroll
     for (int e = 0; e < 16; ++e) {
-      const int key = key0 + 8 * (e >> 2) + 4 * hf + (e & 3);
-      float x = s[e];
-      if constexpr (FMT != kBf16) x *= kse[e];
-      const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(x, a.c_log2, -ml.x)) * ml.y;
-      sum[e] += key <= last && ml.y > 0.0f ? p : 0.0f;
+      kse[x][e] = FMT == kBf16 ? a.c_log2 : __shfl(ks, 8 * (e >> 2) + 4 * hf + (e & 3), 64) * a.c_log2;
+      sum[x][e] = 0.0f;
     }
   }
+  // rows that see the first of the workgroup's keys: from token wg_key - len on
+  const int first = max(0, wg_key - sq.len) * a.g.g / 32, end = (rows + 31) / 32;
+  const int sr = threadIdx.x >> 3, sc = (threadIdx.x & 7) * 2;   // the row and chunks this thread stages
+  v4u g0, g1;
+  float2 gs;
+  auto load = [&](int tile) {
+    const int r = tile * 32 + sr, rr = min(r, rows - 1), i = rr / a.g.g;
+    const size_t qrow = (size_t)(sq.t0 + i) * a.g.Hq + (size_t)j * a.g.g + (rr - i * a.g.g);
+    const v4u* src = reinterpret_cast<const v4u*>(a.q + qrow * kHeadDim);
+    g0 = src[sc];
+    g1 = src[sc + 1];
+    gs = a.stat[qrow];
+    if (r >= rows) gs.y = 0.0f;
+  };
+  auto store = [&](int buf) {
+    qs[buf][sr * 16 + (sc ^ (sr & 15))] = g0;
+    qs[buf][sr * 16 + ((sc + 1) ^ (sr & 15))] = g1;
+    if (sc == 0) ss[buf][sr] = gs;
+  };
+  load(first);
+  store(first & 1);
+  for (int tile = first; tile < end; ++tile) {
+    if (tile + 1 < end) load(tile + 1);
+    __syncthreads();
+    const int buf = tile & 1;
+    v16f s[KW];
 #pragma unroll
-  for (int e = 0; e < 16; ++e) {
-    float x = sum[e];
+    for (int x = 0; x < KW; ++x)
 #pragma unroll
-    for (int o = 16; o >= 1; o >>= 1) x += __shfl_xor(x, o, 64);
-    const int key = key0 + 8 * (e >> 2) + 4 * hf + (e & 3);
-    if (n == 0 && key < sq.n_kv) add_mass(a, b, j, key, x);
+      for (int e = 0; e < 16; ++e) s[x][e] = 0.0f;
+#pragma unroll
+    for (int c = 0; c < 8; ++c) {
+      const v8bf q = __builtin_bit_cast(v8bf, qs[buf][n * 16 + ((2 * c + hf) ^ (n & 15))]);
+#pragma unroll
+      for (int x = 0; x < KW; ++x) s[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[x][c], q, s[x], 0, 0, 0);
+    }
+    const float2 ml = ss[buf][n];
+    // the tile's first token sees every key of the wave?
+    const bool cut = key0 + KW * 32 > min(sq.len + tile * 32 / a.g.g + 1, sq.n_kv);
+    const int last = cut ? min(sq.len + min(tile * 32 + n, rows - 1) / a.g.g, sq.n_kv - 1) : 0x7fffffff;
+#pragma unroll
+    for (int x = 0; x < KW; ++x)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        float z = s[x][e];
+        if (cut) z = key0 + x * 32 + 8 * (e >> 2) + 4 * hf + (e & 3) <= last ? z : -INFINITY;
+        sum[x][e] = __builtin_fmaf(__builtin_amdgcn_exp2f(__builtin_fmaf(z, kse[x][e], -ml.x)), ml.y, sum[x][e]);
+      }
+    if (tile + 1 < end) store((tile + 1) & 1);
   }
+#pragma unroll
+  for (int x = 0; x < KW; ++x)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      float v = sum[x][e];
+#pragma unroll
+      for (int o = 16; o >= 1; o >>= 1) v += __shfl_xor(v, o, 64);
+      const int key = key0 + x * 32 + 8 * (e >> 2) + 4 * hf + (e & 3);
+      if (n != 0 || key >= sq.n_kv) continue;
+      const int p = page_of(a.g, b, key);
+      if (p < 0) continue;
+      float* m = a.mass + pool_row(a.g, p, j, key);
+      *m = a.mass_mode == HYQ_MASS_ADD ? *m + v : v;
+    }
 }
 
 // ---------------------------------------------------------------------------
@@ -780,6 +854,8 @@ struct Plan {
   size_t part, logit, stat;   // workspace bytes
   size_t total() const { return part + logit + stat; }
 };
+
+constexpr int kMassWide = 256;   // workgroups from which a wave of the masses owns 64 keys
 
 size_t up256(size_t x) { return (x + 255) & ~(size_t)255; }
 
@@ -804,7 +880,7 @@ Plan plan_of(const hyq_pcache& c, const hyq_pbatch& b, int mass) {
   const size_t qrows = (size_t)b.T * c.Hq;
   p.part = up256((size_t)S * qrows * kPart * 4);
   if (mass) {
-    p.stat = up256(qrows * sizeof(float2));
+    if (p.many) p.stat = up256(qrows * sizeof(float2));
     if (p.few) {
       p.logit_stride = (int)(units * kUnit);
       p.logit = up256((size_t)heads * kFewRows * p.logit_stride * 4);
@@ -819,14 +895,17 @@ hipError_t launch(const Plan& p, const AttnArgs& a, hipStream_t st) {
   if (p.few) paged_few_kernel<FMT><<<heads * p.S_few, kFewThreads, 0, st>>>(a);
   if (p.many)
     paged_many_kernel<FMT><<<heads * p.row_tiles * p.S_many, kManyThreads, 0, st>>>(a, p.row_tiles);
-  if (p.join_few || p.join_many)
-    paged_join_kernel<<<(unsigned)(a.g.T * a.g.Hq), kJoinThreads, 0, st>>>(a);
-  if (a.mass_mode != HYQ_MASS_NONE) {
-    if (p.few)
-      paged_few_mass_kernel<<<dim3(heads, (unsigned)((p.n_kv + kMassThreads - 1) / kMassThreads)),
-                              kMassThreads, 0, st>>>(a);
-    if (p.many)
-      paged_many_mass_kernel<FMT><<<dim3(heads, (unsigned)((p.n_kv + 127) / 128)), kMassThreads, 0, st>>>(a);
+  const bool mass = a.mass_mode != HYQ_MASS_NONE;
+  if (p.join_few) {
+    const unsigned keys = mass ? (unsigned)((p.n_kv + kMassKeys - 1) / kMassKeys) : 0u;
+    paged_few_finish_kernel<<<dim3(heads, kFewRows + keys), kJoinThreads, 0, st>>>(a);
+  }
+  if (p.join_many) paged_join_kernel<<<(unsigned)(a.g.T * a.g.Hq), kJoinThreads, 0, st>>>(a);
+  if (p.many && mass) {
+    if ((int64_t)heads * ((p.n_kv + 255) / 256) >= kMassWide)
+      paged_many_mass_kernel<FMT, 2><<<dim3(heads, (unsigned)((p.n_kv + 255) / 256)), kMassThreads, 0, st>>>(a);
+    else
+      paged_many_mass_kernel<FMT, 1><<<dim3(heads, (unsigned)((p.n_kv + 127) / 128)), kMassThreads, 0, st>>>(a);
   }
   return hipGetLastError();
 }

@@ -44,12 +44,12 @@ __device__ __forceinline__ int seq_of_token(const PagedGeom& a, int t) {
   return b < a.B && a.cu[b] <= t ? b : -1;
 }
 
-// Page that holds slot n of sequence b, -1 where the table has none.
+// Page that holds slot n of sequence b, -1 where the table has none.  No
+// branch, so that several lookups are in flight at once.
 __device__ __forceinline__ int page_of(const PagedGeom& a, int b, int n) {
   const int i = n >> a.page_log2;
-  if (i >= a.max_pages) return -1;
-  const int p = a.table[(size_t)b * a.max_pages + i];
-  return (unsigned)p < (unsigned)a.n_pages ? p : -1;
+  const int p = a.table[(size_t)b * a.max_pages + min(i, a.max_pages - 1)];
+  return i < a.max_pages && (unsigned)p < (unsigned)a.n_pages ? p : -1;
 }
 
 // Row of slot n in page p, head j (in rows of the pool).
