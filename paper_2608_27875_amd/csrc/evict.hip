@@ -14,7 +14,8 @@ namespace {
 
 constexpr int kSelThreads = 1024, kSelWaves = kSelThreads / 64;
 constexpr int kChunk = kSelThreads * 4;   // slots of one float4 per thread
-constexpr int kBins = 2048;
+constexpr int kBins = 2048, kCopies = 4;
+constexpr int kMaxHeld = 8;   // chunks whose keys fit the registers
 constexpr int kMoveThreads = 256, kMoveRows = kMoveThreads / 16;
 
 struct EvictArgs {
@@ -32,28 +33,32 @@ __device__ __forceinline__ int slots_of(const EvictArgs& a, int b) {
   return (int)min((int64_t)min(max(a.g.lens[b], 0), a.g.max_len), cap);
 }
 
-// Order keys of the four slots from n0 on (n0 a multiple of 4, so in one
-// page): recent slots above every mass, NaN and missing pages below.
-__device__ __forceinline__ void keys4(const EvictArgs& a, int b, int j, int n0, int n, uint32_t (&k)[4]) {
-  float4 m = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-  const int p = n0 < n ? page_of(a.g, b, n0) : -1;
-  if (p >= 0) m = *reinterpret_cast<const float4*>(a.mass + pool_row(a.g, p, j, n0));
-  const float f[4] = {m.x, m.y, m.z, m.w};
-#pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    const uint32_t u = p < 0 || f[e] != f[e] ? 0u : order_key(f[e]);
-    k[e] = n0 + e >= n - a.recent ? 0xffffffffu : u;
-  }
+// Inclusive sum over the lanes of a wave (row shifts, then the last lanes of
+// rows 0 and 2 into rows 1 and 3, then of the lower half into the upper).
+__device__ __forceinline__ uint32_t wave_scan(uint32_t x) {
+  x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x111, 0xf, 0xf, false);
+  x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x112, 0xf, 0xf, false);
+  x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x114, 0xf, 0xf, false);
+  x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x118, 0xf, 0xf, false);
+  x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x142, 0xa, 0xf, false);
+  x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x143, 0xc, 0xf, false);
+  return x;
 }
 
-// C > 0: up to C chunks of slots, their keys in registers; C = 0: any number,
-// read again for every pass.
-template <int C>
+// Wave w holds 256 C consecutive slots of each group of C chunks, lane l the
+// four from 256 c + 4 l on for every c (one group unless there are more slots
+// than kMaxHeld chunks; their keys are then read again for every pass).  Order
+// keys: recent slots above every mass; NaN, missing pages and slots past the
+// last below (those are the last equals, and m <= n of them are taken).
+template <int C, bool MORE>
 __global__ void __launch_bounds__(kSelThreads)
 evict_select_kernel(EvictArgs a) {
-  __shared__ uint32_t hist[kBins];
-  __shared__ uint32_t wsum[2][kSelWaves];
+  // kCopies counts of each bin, by lane: masses crowd into few exponents, and
+  // equal bins of a wave are added one after the other
+  __shared__ uint4 hist[kBins];
+  __shared__ uint32_t wsum[kSelWaves];
   __shared__ uint32_t found[2];   // bin, count above it
+  uint32_t* const h32 = reinterpret_cast<uint32_t*>(hist);
   const int bj = blockIdx.x, b = bj / a.g.Hkv, j = bj - b * a.g.Hkv;
   const int n = slots_of(a, b), m = min(n, a.budget);
   const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
@@ -64,51 +69,53 @@ evict_select_kernel(EvictArgs a) {
     for (int i = tid; i < n; i += kSelThreads) keep[i] = i;
     return;
   }
-  const int nc = (n + kChunk - 1) / kChunk;
-  uint32_t key[C > 0 ? C : 1][4];
-  if constexpr (C > 0) {
+  const int groups = MORE ? (n + C * kChunk - 1) / (C * kChunk) : 1;
+  uint32_t key[C * 4];
+  auto load = [&](int grp) {
+    const int n0 = (grp * kSelWaves + w) * C * 256 + lane * 4;
+    float4 f[C];
+    int p[C];
 #pragma unroll
-    for (int c = 0; c < C; ++c) keys4(a, b, j, c * kChunk + tid * 4, n, key[c]);
-  }
-  // body(c, keys of this thread's 4 slots, first of them)
-  auto each = [&](auto body) {
-    if constexpr (C > 0) {
+    for (int c = 0; c < C; ++c) {   // 4 slots from a multiple of 4 on: one page
+      p[c] = page_of(a.g, b, n0 + 256 * c);
+      f[c] = *reinterpret_cast<const float4*>(a.mass + pool_row(a.g, max(p[c], 0), j, n0 + 256 * c));
+    }
 #pragma unroll
-      for (int c = 0; c < C; ++c)
-        if (c < nc) body(key[c], c * kChunk + tid * 4);
-    } else {
-      for (int c = 0; c < nc; ++c) {
-        keys4(a, b, j, c * kChunk + tid * 4, n, key[0]);
-        body(key[0], c * kChunk + tid * 4);
+    for (int c = 0; c < C; ++c) {
+      const float x[4] = {f[c].x, f[c].y, f[c].z, f[c].w};
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int slot = n0 + 256 * c + e;
+        const uint32_t u = p[c] < 0 || x[e] != x[e] || slot >= n ? 0u : order_key(x[e]);
+        key[4 * c + e] = slot >= n - a.recent && slot < n ? 0xffffffffu : u;
       }
     }
   };
+  if (!MORE) load(0);
   // the m-th largest key, bits from the top; `left` of the keys that share the
   // bits found so far are still wanted
   uint32_t prefix = 0, left = (uint32_t)m;
   int shift = 32;
   for (int pass = 0; pass < 3; ++pass) {
     const int bits = pass < 2 ? 11 : 10, below = shift - bits;
-    for (int i = tid; i < kBins; i += kSelThreads) hist[i] = 0u;
+    for (int i = tid; i < kBins; i += kSelThreads) hist[i] = make_uint4(0u, 0u, 0u, 0u);
     __syncthreads();
-    each([&](const uint32_t (&k)[4], int n0) {
+    for (int grp = 0; grp < groups; ++grp) {
+      if (MORE) load(grp);
 #pragma unroll
-      for (int e = 0; e < 4; ++e)
-        if (n0 + e < n && (pass == 0 || (k[e] >> shift) == prefix))
-          atomicAdd(&hist[(k[e] >> below) & ((1u << bits) - 1)], 1u);
-    });
+      for (int e = 0; e < 4 * C; ++e)
+        if (pass == 0 || (key[e] >> shift) == prefix)
+          atomicAdd(&h32[((key[e] >> below) & ((1u << bits) - 1)) * kCopies + (lane & (kCopies - 1))], 1u);
+    }
     __syncthreads();
     // thread t takes the bins 2047 - 2t and 2046 - 2t: counts from the top
-    const uint32_t c0 = hist[kBins - 1 - 2 * tid], c1 = hist[kBins - 2 - 2 * tid];
-    uint32_t sum = c0 + c1;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const uint32_t up = __shfl_up(sum, o, 64);
-      if (lane >= o) sum += up;
-    }
-    if (lane == 63) wsum[0][w] = sum;
+    const uint4 u0 = hist[kBins - 1 - 2 * tid], u1 = hist[kBins - 2 - 2 * tid];
+    const uint32_t c0 = u0.x + u0.y + u0.z + u0.w, c1 = u1.x + u1.y + u1.z + u1.w;
+    uint32_t sum = wave_scan(c0 + c1);
+    if (lane == 63) wsum[w] = sum;
     __syncthreads();
-    for (int x = 0; x < w; ++x) sum += wsum[0][x];
+#pragma unroll
+    for (int x = 0; x < kSelWaves; ++x) sum += x < w ? wsum[x] : 0u;
     const uint32_t before = sum - c0 - c1;   // keys in higher bins
     if (before < left && sum >= left) {
       const bool second = before + c0 < left;
@@ -119,80 +126,104 @@ evict_select_kernel(EvictArgs a) {
     prefix = (prefix << bits) | found[0];
     left -= found[1];
     shift = below;
-    __syncthreads();
   }
-  // slots in order: a kept one's place is the number of larger keys before it
-  // plus the equal ones before it, of which the first `left` are kept
-  uint32_t gt0 = 0, eq0 = 0;   // of all chunks before
-  each([&](const uint32_t (&k)[4], int n0) {
-    const uint64_t lower = (1ull << lane) - 1;
-    uint32_t gt = 0, eq = 0, wgt = 0, weq = 0;
-    bool is_gt[4], is_eq[4];
+  // a kept slot's place is the number of larger keys before it plus the equal
+  // ones before it, of which the first `left` are kept
+  uint32_t gt0 = 0, eq0 = 0;   // of all groups before
+  for (int grp = 0; grp < groups; ++grp) {
+    if (MORE) load(grp);
+    // counts of the lane's four slots per chunk, three chunks to a word (a
+    // wave's are at most 256), scanned over the lanes
+    constexpr int kWords = (C + 2) / 3;
+    uint32_t gw[kWords] = {}, ew[kWords] = {}, gs[kWords], es[kWords];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      is_gt[e] = n0 + e < n && k[e] > prefix;
-      is_eq[e] = n0 + e < n && k[e] == prefix;
-      const uint64_t bg = __ballot(is_gt[e]), be = __ballot(is_eq[e]);
-      gt += __popcll(bg & lower);
-      eq += __popcll(be & lower);
-      wgt += __popcll(bg);
-      weq += __popcll(be);
+    for (int c = 0; c < C; ++c)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        gw[c / 3] += key[4 * c + e] > prefix ? 1u << (10 * (c % 3)) : 0u;
+        ew[c / 3] += key[4 * c + e] == prefix ? 1u << (10 * (c % 3)) : 0u;
+      }
+    uint32_t all_g = 0, all_e = 0, before_g[C], before_e[C];
+#pragma unroll
+    for (int x = 0; x < kWords; ++x) {
+      gs[x] = wave_scan(gw[x]);
+      es[x] = wave_scan(ew[x]);
     }
-    if (lane == 0) {
-      wsum[0][w] = wgt;
-      wsum[1][w] = weq;
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      const int sh = 10 * (c % 3);
+      before_g[c] = all_g + (((gs[c / 3] - gw[c / 3]) >> sh) & 1023u);
+      before_e[c] = all_e + (((es[c / 3] - ew[c / 3]) >> sh) & 1023u);
+      all_g += ((uint32_t)__builtin_amdgcn_readlane((int)gs[c / 3], 63) >> sh) & 1023u;
+      all_e += ((uint32_t)__builtin_amdgcn_readlane((int)es[c / 3], 63) >> sh) & 1023u;
     }
+    if (lane == 0) wsum[w] = all_g | all_e << 16;   // a group holds at most 2^15 slots
     __syncthreads();
-    uint32_t all_gt = 0, all_eq = 0;
+    uint32_t lower = 0, all = 0;
 #pragma unroll
     for (int x = 0; x < kSelWaves; ++x) {
-      const uint32_t g1 = wsum[0][x], e1 = wsum[1][x];
-      if (x < w) {
-        gt += g1;
-        eq += e1;
-      }
-      all_gt += g1;
-      all_eq += e1;
+      const uint32_t v = wsum[x];
+      lower += x < w ? v : 0u;
+      all += v;
     }
-    gt += gt0;
-    eq += eq0;
+    const int n0 = (grp * kSelWaves + w) * C * 256 + lane * 4;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      if (is_gt[e] || (is_eq[e] && eq < left)) keep[gt + min(eq, left)] = n0 + e;
-      gt += is_gt[e];
-      eq += is_eq[e];
+    for (int c = 0; c < C; ++c) {
+      uint32_t gt = gt0 + (lower & 0xffffu) + before_g[c], eq = eq0 + (lower >> 16) + before_e[c];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const bool is_gt = key[4 * c + e] > prefix, is_eq = key[4 * c + e] == prefix;
+        if (is_gt || (is_eq && eq < left)) keep[gt + min(eq, left)] = n0 + 256 * c + e;
+        gt += is_gt;
+        eq += is_eq;
+      }
     }
-    gt0 += all_gt;
-    eq0 += all_eq;
+    gt0 += all & 0xffffu;
+    eq0 += all >> 16;
     __syncthreads();
-  });
+  }
 }
 
-// Workgroup (rows, bj): 16 kept rows at a time, 16 lanes to a row.  A row of a
-// missing page becomes zero.
+// Workgroup (rows, bj): 16 lanes to a row, kMoveEach rows in flight per lane.
+// A row of a missing page becomes zero.
+constexpr int kMoveEach = 4;
 template <typename W>   // a lane's part of a row: uint4 (bf16) or uint2 (codes)
 __global__ void __launch_bounds__(kMoveThreads)
 evict_move_kernel(EvictArgs a) {
   const int bj = blockIdx.y, b = bj / a.g.Hkv, j = bj - b * a.g.Hkv;
   const int m = min(slots_of(a, b), a.budget);
-  const int i = blockIdx.x * kMoveRows + (int)(threadIdx.x >> 4), sub = threadIdx.x & 15;
-  if (i >= m) return;
-  const int ni = i >> a.g.page_log2;
-  const int np = a.new_table[(size_t)b * a.new_pages + ni];
-  if ((unsigned)np >= (unsigned)a.g.n_pages) return;
-  const int from = a.keep[(size_t)bj * a.budget + i];
-  const int p = page_of(a.g, b, from);
-  const size_t src = pool_row(a.g, max(p, 0), j, from), dst = pool_row(a.g, np, j, i);
-  W kw = {}, vw = {};
-  if (p >= 0) {
-    kw = reinterpret_cast<const W*>(a.k + src * a.row_bytes)[sub];
-    vw = reinterpret_cast<const W*>(a.v + src * a.row_bytes)[sub];
+  const int i0 = blockIdx.x * (kMoveRows * kMoveEach) + (int)(threadIdx.x >> 4), sub = threadIdx.x & 15;
+  if (i0 >= m) return;
+  size_t src[kMoveEach], dst[kMoveEach];
+  bool there[kMoveEach], take[kMoveEach];
+#pragma unroll
+  for (int e = 0; e < kMoveEach; ++e) {
+    const int i = i0 + e * kMoveRows, at = min(i, m - 1);
+    const int np = a.new_table[(size_t)b * a.new_pages + (at >> a.g.page_log2)];
+    const int from = a.keep[(size_t)bj * a.budget + at];
+    const int p = page_of(a.g, b, from);
+    there[e] = p >= 0;
+    take[e] = i < m && (unsigned)np < (unsigned)a.g.n_pages;
+    src[e] = pool_row(a.g, max(p, 0), j, from);
+    dst[e] = pool_row(a.g, take[e] ? np : 0, j, at);
   }
-  reinterpret_cast<W*>(a.k + dst * a.row_bytes)[sub] = kw;
-  reinterpret_cast<W*>(a.v + dst * a.row_bytes)[sub] = vw;
-  if (sub == 0) a.mass[dst] = p >= 0 ? a.mass[src] : 0.0f;
-  if (a.ks && sub == 1) a.ks[dst] = p >= 0 ? a.ks[src] : 0.0f;
-  if (a.vs && sub == 2) a.vs[dst] = p >= 0 ? a.vs[src] : 0.0f;
+  W kw[kMoveEach], vw[kMoveEach];
+  // lanes 0, 1, 2 also carry the row's mass and scales
+  float* side = sub == 0 ? a.mass : sub == 1 ? a.ks : sub == 2 ? a.vs : nullptr;
+  float f[kMoveEach];
+#pragma unroll
+  for (int e = 0; e < kMoveEach; ++e) {
+    kw[e] = reinterpret_cast<const W*>(a.k + src[e] * a.row_bytes)[sub];
+    vw[e] = reinterpret_cast<const W*>(a.v + src[e] * a.row_bytes)[sub];
+    f[e] = side ? side[src[e]] : 0.0f;
+  }
+#pragma unroll
+  for (int e = 0; e < kMoveEach; ++e) {
+    if (!take[e]) continue;
+    reinterpret_cast<W*>(a.k + dst[e] * a.row_bytes)[sub] = there[e] ? kw[e] : W{};
+    reinterpret_cast<W*>(a.v + dst[e] * a.row_bytes)[sub] = there[e] ? vw[e] : W{};
+    if (side) side[dst[e]] = there[e] ? f[e] : 0.0f;
+  }
 }
 
 }  // namespace
@@ -223,14 +254,14 @@ hipError_t launch_evict(const hyq_pcache& c, int B, const int32_t* lens, const i
   a.new_lens = new_lens;
   const unsigned heads = (unsigned)(B * c.Hkv);
   const int chunks = (max_len + kChunk - 1) / kChunk;
-  if (chunks <= 1) evict_select_kernel<1><<<heads, kSelThreads, 0, st>>>(a);
-  else if (chunks <= 2) evict_select_kernel<2><<<heads, kSelThreads, 0, st>>>(a);
-  else if (chunks <= 4) evict_select_kernel<4><<<heads, kSelThreads, 0, st>>>(a);
-  else if (chunks <= 8) evict_select_kernel<8><<<heads, kSelThreads, 0, st>>>(a);
-  else evict_select_kernel<0><<<heads, kSelThreads, 0, st>>>(a);
+  if (chunks <= 1) evict_select_kernel<1, false><<<heads, kSelThreads, 0, st>>>(a);
+  else if (chunks <= 2) evict_select_kernel<2, false><<<heads, kSelThreads, 0, st>>>(a);
+  else if (chunks <= 4) evict_select_kernel<4, false><<<heads, kSelThreads, 0, st>>>(a);
+  else if (chunks <= kMaxHeld) evict_select_kernel<kMaxHeld, false><<<heads, kSelThreads, 0, st>>>(a);
+  else evict_select_kernel<kMaxHeld, true><<<heads, kSelThreads, 0, st>>>(a);
   const int rows = budget < max_len ? budget : max_len;
   if (rows > 0) {
-    const dim3 grid((unsigned)((rows + kMoveRows - 1) / kMoveRows), heads);
+    const dim3 grid((unsigned)((rows + kMoveRows * kMoveEach - 1) / (kMoveRows * kMoveEach)), heads);
     if (c.bits_kv == 16) evict_move_kernel<uint4><<<grid, kMoveThreads, 0, st>>>(a);
     else evict_move_kernel<uint2><<<grid, kMoveThreads, 0, st>>>(a);
   }
