@@ -530,28 +530,22 @@ def hyq_decode_attn_noalloc(cache: DecodeCache, q, out, softmax_scale: float | N
 # paged serving: norms and rotation, the paged cache, its attention, eviction
 # --------------------------------------------------------------------------
 
-def _on_device(device, stream):
-    """The stream of a call on ``device`` (which need not be the current one)
-    and the context to make the call in."""
+def _call(device, stream, fn, *args):
+    """fn(*args, stream) with ``device`` current (the tensors need not be on the
+    caller's current device), on ``stream`` or the device's current one."""
     torch = _torch()
     if device.type != "cuda":
         raise ValueError("tensors must be on a GPU")
-    if stream is not None:
+    if stream is None:
+        st = torch._C._cuda_getCurrentRawStream(device.index)
+    else:
         if getattr(stream, "device", device) != device:
             raise ValueError(f"the stream is on {stream.device}, the tensors are on {device}")
-    else:
-        stream = torch._C._cuda_getCurrentRawStream(device.index)
-    return _stream(stream), torch.cuda.device(device)
-
-
-def _call(device, stream, fn, *args):
-    """fn(*args, stream) with ``device`` current."""
-    torch = _torch()
-    st, guard = _on_device(device, stream)
-    if torch.cuda.current_device() == device.index:
+        st = _stream(stream)
+    if torch._C._cuda_getDevice() == device.index:
         _check(fn(*args, st))
     else:
-        with guard:
+        with torch.cuda.device(device):
             _check(fn(*args, st))
 
 
@@ -578,18 +572,18 @@ def _row_args(t, name, T, heads, D, device):
     """(pointer, elements from token to token) of rows [T, heads, D]."""
     if t is None:
         return None, 0
-    if tuple(t.shape) != (T, heads, D):
+    if t.shape != (T, heads, D):
         raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {(T, heads, D)}")
     if t.dtype != _torch().bfloat16:
         raise TypeError(f"{name}: dtype {t.dtype}, expected bfloat16")
     if t.device != device:
         raise ValueError(f"{name} is on {t.device}, expected {device}")
-    if t.numel() == 0:
+    if T == 0:
         return None, heads * D
-    if t.stride(2) != 1 or (heads > 1 and t.stride(1) != D):
+    st = t.stride()
+    if st[2] != 1 or (heads > 1 and st[1] != D):
         raise ValueError(f"{name}: the heads of a token must be contiguous")
-    stride = t.stride(0) if T > 1 else heads * D
-    return t.data_ptr(), stride
+    return t.data_ptr(), st[0] if T > 1 else heads * D
 
 
 def _rope_for(rope: Rope, device):
@@ -724,7 +718,7 @@ def hyq_paged_attn(cache: PagedCache, batch: PagedBatch, q, out, softmax_scale: 
     torch = _torch()
     c, dev, T = cache.c, cache.device, q.shape[0]
     want = (T, c.Hq, c.D)
-    if tuple(q.shape) != want or tuple(out.shape) != want:
+    if q.shape != want or out.shape != want:
         raise ValueError(f"q and out have shapes {tuple(q.shape)} and {tuple(out.shape)}, "
                          f"expected {want}")
     n = T * c.Hq * c.D

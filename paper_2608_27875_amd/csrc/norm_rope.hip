@@ -40,15 +40,23 @@ struct RopeArgs {
   float *pks, *pvs, *mass;
 };
 
+// x of the lane `N` places on in the same 16 (cyclic).
+template <int N>
+__device__ __forceinline__ float rotate16(float x) {
+  return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x120 + N, 0xf, 0xf, false));
+}
+// Sum and maximum over a row's 16 lanes, the same bits in each.
 __device__ __forceinline__ float sum16(float v) {
-#pragma unroll
-  for (int o = 8; o >= 1; o >>= 1) v += __shfl_xor(v, o, 64);
-  return v;
+  v += rotate16<8>(v);
+  v += rotate16<4>(v);
+  v += rotate16<2>(v);
+  return v + rotate16<1>(v);
 }
 __device__ __forceinline__ float max16(float v) {
-#pragma unroll
-  for (int o = 8; o >= 1; o >>= 1) v = fmaxf(v, __shfl_xor(v, o, 64));
-  return v;
+  v = fmaxf(v, rotate16<8>(v));
+  v = fmaxf(v, rotate16<4>(v));
+  v = fmaxf(v, rotate16<2>(v));
+  return fmaxf(v, rotate16<1>(v));
 }
 
 __device__ __forceinline__ void widen8(const uint4& w, float (&x)[8]) {
@@ -64,6 +72,29 @@ __device__ __forceinline__ uint32_t pack2(float a, float b) {
   typedef __bf16 v2bf __attribute__((ext_vector_type(2)));
   const v2bf r = {(__bf16)a, (__bf16)b};
   return __builtin_bit_cast(uint32_t, r);
+}
+
+// Eight codes of x / s (s > 0), one per byte; the correctly rounded quotient.
+template <int FMT>
+__device__ __forceinline__ void codes8f(const float (&x)[8], float s, float c, uint32_t (&o)[2]) {
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    float y[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) y[e] = x[4 * h + e] / s;
+    if constexpr (FMT == HYQ_FMT_FP8) {   // two conversions fill the word
+#pragma unroll
+      for (int e = 0; e < 4; ++e) y[e] = fminf(fmaxf(y[e], -448.0f), 448.0f);
+      int v = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
+      v = __builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], v, true);
+      o[h] = (uint32_t)v;
+    } else {
+      uint32_t v = 0;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v |= (uint32_t)(code_int(y[e], c) & 0xff) << (8 * e);
+      o[h] = v;
+    }
+  }
 }
 
 // PAGES: 0 dense outputs, 16 bf16 pages, 8 pages of codes FMT.  Workgroup
@@ -94,72 +125,83 @@ norm_rope_kernel(RopeArgs a, int passes) {
   }
   __syncthreads();
   const int rows = a.Hq + 2 * a.Hkv;
+  // dense outputs: rows of sequence b = t / L
+  size_t q_at = (size_t)t * a.Hq, kv_at = 0;
+  int L = 1;
+  if (PAGES == 0) {
+    const int b = t / a.L, i = t - b * a.L;
+    L = a.L;
+    q_at = (size_t)b * a.Hq * L + i;
+    kv_at = (size_t)b * a.Hkv * L + i;
+  }
   for (int p = 0; p < passes; ++p) {
     const int r = (blockIdx.y * passes + p) * kRowsPerPass + (int)(threadIdx.x >> 4);
     const bool is_q = r < a.Hq, is_v = r >= a.Hq + a.Hkv;
     const int h = is_q ? r : is_v ? r - a.Hq - a.Hkv : r - a.Hq;
     const uint16_t* src = is_q ? a.x.q : is_v ? a.x.v : a.x.k;
     const bool live = r < rows && src != nullptr && (PAGES == 0 || is_q || page >= 0);
-    float x[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
     uint4 raw = make_uint4(0u, 0u, 0u, 0u);
     if (live) {
       const int64_t stride = is_q ? a.x.q_stride : is_v ? a.x.v_stride : a.x.k_stride;
       raw = reinterpret_cast<const uint4*>(src + (size_t)t * stride + h * kHeadDim)[sub];
-      widen8(raw, x);
     }
-    const uint16_t* w = is_q ? a.qw : is_v ? nullptr : a.kw;
-    float ss = 0.0f;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) ss = __builtin_fmaf(x[e], x[e], ss);
-    ss = sum16(ss);
-    if (w) {
-      const float inv = 1.0f / sqrtf(ss * (1.0f / kHeadDim) + a.eps);
-      float wf[8];
-      widen8(reinterpret_cast<const uint4*>(w)[sub], wf);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) x[e] *= inv * wf[e];
-    }
-    if (a.interleaved) {
-      if (!is_v && sub * 8 < a.rot) {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float2 f = cs[sub * 4 + e];
-          const float u = x[2 * e], v = x[2 * e + 1];
-          x[2 * e] = u * f.x - v * f.y;
-          x[2 * e + 1] = v * f.x + u * f.y;
-        }
-      }
-    } else {
-      const int half = a.rot >> 4;   // lanes of the first half of the pairs
-      const bool second = sub >= half;
-      const bool turned = !is_v && sub < 2 * half;
-      const int lane = threadIdx.x & 63;
-      const int mate = turned ? (second ? lane - half : lane + half) : lane;
-      float y[8];
-#pragma unroll
-      for (int e = 0; e < 8; ++e) y[e] = __shfl(x[e], mate, 64);
-      if (turned) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const float2 f = cs[(second ? sub - half : sub) * 8 + e];
-          x[e] = second ? x[e] * f.x + y[e] * f.y : x[e] * f.x - y[e] * f.y;
-        }
-      }
-    }
+    float x[8];
+    widen8(raw, x);
     uint4 o = raw;   // values are copied as they are
-    if (!is_v) o = make_uint4(pack2(x[0], x[1]), pack2(x[2], x[3]), pack2(x[4], x[5]), pack2(x[6], x[7]));
-    if (PAGES == 0 || is_q) {
-      if (!live) continue;
-      size_t row;
-      uint16_t* dst = a.Q;
-      if (PAGES) {
-        row = (size_t)t * a.Hq + h;
-      } else {
-        const int b = t / a.L, i = t - b * a.L;
-        row = ((size_t)b * (is_q ? a.Hq : a.Hkv) + h) * a.L + i;
-        if (!is_q) dst = is_v ? a.V : a.K;
+    if (__ballot(!is_v)) {   // a wave of value rows has nothing to work out
+      const uint16_t* w = is_q ? a.qw : a.kw;
+      if (w && !is_v) {
+        uint4 wr = reinterpret_cast<const uint4*>(w)[sub];
+        float ss = 0.0f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) ss = __builtin_fmaf(x[e], x[e], ss);
+        ss = sum16(ss);
+        const float inv = 1.0f / sqrtf(ss * (1.0f / kHeadDim) + a.eps);
+        float wf[8];
+        widen8(wr, wf);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] *= inv * wf[e];
       }
-      reinterpret_cast<uint4*>(dst + row * kHeadDim)[sub] = o;
+      if (a.interleaved) {
+        if (!is_v && sub * 8 < a.rot) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float2 f = cs[sub * 4 + e];
+            const float u = x[2 * e], v = x[2 * e + 1];
+            x[2 * e] = u * f.x - v * f.y;
+            x[2 * e + 1] = v * f.x + u * f.y;
+          }
+        }
+      } else {
+        const int half = a.rot >> 4;   // lanes of the first half of the pairs
+        const bool second = sub >= half;
+        const bool turned = !is_v && sub < 2 * half;
+        float y[8];   // the other entries of this lane's pairs
+        if (half == 8) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) y[e] = rotate16<8>(x[e]);
+        } else {
+          const int lane = threadIdx.x & 63;
+          const int mate = turned ? (second ? lane - half : lane + half) : lane;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) y[e] = __shfl(x[e], mate, 64);
+        }
+        if (turned) {
+          const float sign = second ? 1.0f : -1.0f;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const float2 f = cs[(second ? sub - half : sub) * 8 + e];
+            x[e] = x[e] * f.x + y[e] * (sign * f.y);
+          }
+        }
+      }
+      if (!is_v)
+        o = make_uint4(pack2(x[0], x[1]), pack2(x[2], x[3]), pack2(x[4], x[5]), pack2(x[6], x[7]));
+    }
+    if (PAGES == 0 || is_q) {
+      uint16_t* dst = is_q ? a.Q : is_v ? a.V : a.K;
+      const size_t row = (is_q ? q_at : kv_at) + (size_t)h * L;
+      if (live) reinterpret_cast<uint4*>(dst + row * kHeadDim)[sub] = o;
     } else {
       const size_t row = pool_row(a.g, max(page, 0), min(h, a.Hkv - 1), slot);
       if (PAGES == 16) {
@@ -171,11 +213,7 @@ norm_rope_kernel(RopeArgs a, int passes) {
         for (int e = 0; e < 8; ++e) m = fmaxf(m, fabsf(x[e]));
         const float s = max16(m) / C;
         uint32_t cw[2] = {0u, 0u};
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const uint32_t c = s > 0.0f ? (uint32_t)(quant_code<FMT>(x[e], s, C) & 0xff) : 0u;
-          cw[e >> 2] |= c << (8 * (e & 3));
-        }
+        if (s > 0.0f) codes8f<FMT>(x, s, C, cw);
         if (live) {
           reinterpret_cast<uint2*>((is_v ? a.pv : a.pk) + row * kHeadDim)[sub] =
               make_uint2(cw[0], cw[1]);
@@ -190,7 +228,10 @@ norm_rope_kernel(RopeArgs a, int passes) {
 template <int PAGES, int FMT>
 hipError_t launch(const RopeArgs& a, hipStream_t st) {
   const int groups = (a.Hq + 2 * a.Hkv + kRowsPerPass - 1) / kRowsPerPass;
-  const int passes = groups;
+  // A token's rows go to several workgroups where there are few tokens (16
+  // tokens of 48 rows: 3.7 us in 48 workgroups, 5.5 in 16); otherwise one takes
+  // them all and works out the angles once.
+  const int passes = (int64_t)a.T * groups <= 1024 ? 1 : groups;
   norm_rope_kernel<PAGES, FMT>
       <<<dim3((unsigned)a.T, (unsigned)((groups + passes - 1) / passes)), kRopeThreads, 0, st>>>(a, passes);
   return hipGetLastError();
