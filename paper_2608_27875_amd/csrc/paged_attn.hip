@@ -36,7 +36,7 @@ typedef unsigned v2u __attribute__((ext_vector_type(2)));
 constexpr int kBf16 = -1;            // page format beside HYQ_FMT_INT / HYQ_FMT_FP8 (8-bit codes)
 constexpr int kFewRows = 16;         // rows per KV head of the few-row kernel
 constexpr int kFewThreads = 256, kFewWaves = 4, kUnit = 32;
-constexpr int kRowTile = 128, kKeyTile = 64, kManyThreads = 256;
+constexpr int kKeyTile = 64;         // keys of a tile of the many-row kernel
 constexpr int kPart = kHeadDim + 4;  // floats of a partial: acc[128], max, sum, padding
 constexpr float kLazy = 8.0f;        // rescale only when the maximum grows by more than 2^8
 constexpr float kNever = 3.0e38f;    // the "maximum" of a row that sees nothing: exp2(z - it) is 0
@@ -58,8 +58,15 @@ struct AttnArgs {
   float* part;         // [S][T][Hq][kPart]
   float* logit;        // few rows with mass: [B][Hkv][kFewRows][logit_stride]
   int logit_stride;
+  uint32_t inv_g;      // ceil(2^32 / g) (g > 1): r / g for the rows of a step
   float2* stat;        // many rows with mass: (max, 1 / sum) of every query row [T][Hq]
 };
+
+// Token of row r of a KV head's rows: r / g.  Exact for r < 2^29 (the product
+// is off by less than r g / 2^32 < 1 / g, g <= 8).
+__device__ __forceinline__ int token_of(const AttnArgs& a, int r) {
+  return a.g.g == 1 ? r : (int)__umulhi((uint32_t)r, a.inv_g);
+}
 
 // Four codes (one dword) -> two pairs of bf16, exact (both formats have at
 // most 8 significant bits).
@@ -389,81 +396,70 @@ paged_few_kernel(AttnArgs a) {
 // Many rows.
 // ---------------------------------------------------------------------------
 
-// Tile of 64 keys in LDS: K rows of 16 chunks of 16 bytes, chunk c of row r at
-// c ^ (r & 15); V transposed, channel rows of 8 chunks (8 keys each), chunk c
-// of channel d at c ^ ((d >> 1) & 7).  Both make the 16 lanes of a read phase
-// meet 16 different bank groups.
+// Tiles of 64 keys in LDS, rows of 16 chunks of 16 bytes: chunk c of K row r at
+// c ^ (r & 15), of V row r at c ^ 4 (r & 3).  The first makes the 16 lanes of a
+// read phase (16 rows, one chunk) meet different banks, the second the 32 of a
+// transposing read (4 rows, 4 chunks).
 struct ManyLds {
-  uint4 k[kKeyTile * 16];
-  uint4 v[kHeadDim * 8];
-  float ks[kKeyTile], vs[kKeyTile];
-  uint8_t gone[8];   // 8-key groups whose page is missing
+  v4u k[2][kKeyTile * 16];
+  v4u v[2][kKeyTile * 16];
+  // of K's tiles
+  float ks[2][kKeyTile], vs[2][kKeyTile];
+  uint8_t gone[2][kKeyTile / 4];   // 4-key groups whose page is missing
 };
 
-// What one thread holds of the next tile: eight rows of eight channels.
-// Threads 0..127 carry V (key group tid % 8, channel group tid / 8), 128..255
-// K (key group (tid - 128) / 16, chunk tid % 16).
-template <int FMT>
+// What one thread holds of a tile's K or V: U rows (keys U kg ..) of eight
+// channels (chunk).
+template <int FMT, int U>
 struct Stage {
-  typename Eight<FMT>::type x[8];
-  v4f s[2];
-  int page;
+  typename Eight<FMT>::type x[U];
+  float ks, vs;   // codes: scales of key U kg + chunk % U, loaded with K
+  int page;       // -1: missing
 };
 
-template <int FMT>
-__device__ __forceinline__ void stage_load(Stage<FMT>& g, const AttnArgs& a, int page, int j, int tile,
-                                           int kg, int chunk, bool is_v) {
-  const bool ok = (unsigned)page < (unsigned)a.g.n_pages;
-  g.page = ok ? page : -1;
-  const size_t row = pool_row(a.g, ok ? page : 0, j, tile * kKeyTile + kg * 8);
-  const uint8_t* p = (is_v ? a.v : a.k) + row * row_bytes<FMT>() + chunk * (row_bytes<FMT>() / 16);
+template <int FMT, bool IS_K, int U>
+__device__ __forceinline__ void stage_load(Stage<FMT, U>& g, const AttnArgs& a, int page, int j, int tile,
+                                           int kg, int chunk) {
+  g.page = page;
+  const size_t row = pool_row(a.g, max(page, 0), j, tile * kKeyTile + kg * U);
+  const uint8_t* p = (IS_K ? a.k : a.v) + row * row_bytes<FMT>() + chunk * (row_bytes<FMT>() / 16);
 #pragma unroll
-  for (int e = 0; e < 8; ++e)
+  for (int e = 0; e < U; ++e)
     g.x[e] = *reinterpret_cast<const typename Eight<FMT>::type*>(p + e * row_bytes<FMT>());
-  if constexpr (FMT != kBf16) {
-    const float* sc = (is_v ? a.vs : a.ks) + row;
-    g.s[0] = *reinterpret_cast<const v4f*>(sc);
-    g.s[1] = *reinterpret_cast<const v4f*>(sc + 4);
+  if constexpr (FMT != kBf16 && IS_K) {
+    g.ks = a.ks[row + (chunk & (U - 1))];
+    g.vs = a.vs[row + (chunk & (U - 1))];
   }
 }
 
-template <int FMT>
-__device__ __forceinline__ void stage_store(const Stage<FMT>& g, ManyLds& m, int tile, int n_kv, int kg,
-                                            int chunk, bool is_v) {
-  v4u rows[8];
+template <int FMT, int U>
+__device__ __forceinline__ void store_k(const Stage<FMT, U>& g, ManyLds& m, int buf, int tile, int n_kv,
+                                        int kg, int chunk, float c_log2) {
 #pragma unroll
-  for (int e = 0; e < 8; ++e) rows[e] = to_bf16<FMT>(g.x[e]);
-  if (is_v) {
-    const int there = g.page < 0 ? 0 : n_kv - (tile * kKeyTile + kg * 8);
-    if (there < 8) {
+  for (int e = 0; e < U; ++e) {
+    const int r = kg * U + e;
+    m.k[buf][r * 16 + (chunk ^ (r & 15))] = to_bf16<FMT>(g.x[e]);
+  }
+  if (chunk == 0 && (kg * U) % 4 == 0) m.gone[buf][kg * U / 4] = g.page < 0;
+  if constexpr (FMT != kBf16) {   // finite and positive, so that hidden scores stay -inf
+    const int there = g.page < 0 ? 0 : n_kv - (tile * kKeyTile + kg * U);
+    if (chunk < U) {
+      m.ks[buf][kg * U + chunk] = (chunk < there ? fmaxf(g.ks, 1e-30f) : 1.0f) * c_log2;
+      m.vs[buf][kg * U + chunk] = chunk < there ? g.vs : 0.0f;
+    }
+  }
+}
+
+template <int FMT, int U>
+__device__ __forceinline__ void store_v(const Stage<FMT, U>& g, ManyLds& m, int buf, int tile, int n_kv,
+                                        int kg, int chunk) {
+  const int there = g.page < 0 ? 0 : n_kv - (tile * kKeyTile + kg * U);   // rows nobody owns are zero
 #pragma unroll
-      for (int e = 0; e < 8; ++e)
-        if (e >= there) rows[e] = v4u{0u, 0u, 0u, 0u};
-    }
-#pragma unroll
-    for (int t = 0; t < 8; ++t) {
-      const int d = chunk * 8 + t;
-      reinterpret_cast<v4u*>(m.v)[d * 8 + (kg ^ ((d >> 1) & 7))] = column(rows, t);
-    }
-    if constexpr (FMT != kBf16) {
-      if (chunk == 0) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) m.vs[kg * 8 + e] = e < there ? g.s[e >> 2][e & 3] : 0.0f;
-      }
-    }
-  } else {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const int r = kg * 8 + e;
-      reinterpret_cast<v4u*>(m.k)[r * 16 + (chunk ^ (r & 15))] = rows[e];
-    }
-    if (chunk == 0) {
-      m.gone[kg] = g.page < 0;
-      if constexpr (FMT != kBf16) {
-        *reinterpret_cast<v4f*>(m.ks + kg * 8) = g.s[0];
-        *reinterpret_cast<v4f*>(m.ks + kg * 8 + 4) = g.s[1];
-      }
-    }
+  for (int e = 0; e < U; ++e) {
+    const int r = kg * U + e;
+    v4u x = to_bf16<FMT>(g.x[e]);
+    if (e >= there) x = v4u{0u, 0u, 0u, 0u};
+    m.v[buf][r * 16 + (chunk ^ ((r & 3) << 2))] = x;
   }
 }
 
@@ -472,10 +468,77 @@ __device__ __forceinline__ void stage_store(const Stage<FMT>& g, ManyLds& m, int
 // B operand.
 __device__ __forceinline__ int many_key(int m) { return (m & 0x13) | ((m & 4) << 1) | ((m & 8) >> 1); }
 
-template <int FMT>
-__global__ void __launch_bounds__(kManyThreads, 2)
-paged_many_kernel(AttnArgs a, int tiles) {
-  __shared__ ManyLds lds[2];
+// S^T = K q^T of one tile: s[x][e] is key 32x + 16 (e / 8) + 8 hf + e % 8, row n.
+__device__ __forceinline__ void many_scores(v16f (&s)[2], const v4u* kt, const v8bf (&q)[8], int n, int hf) {
+  const int r = many_key(n);
+  v4u ka[8];
+#pragma unroll
+  for (int c = 0; c < 8; ++c) ka[c] = kt[r * 16 + ((2 * c + hf) ^ (r & 15))];
+#pragma unroll
+  for (int x = 0; x < 2; ++x)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) s[x][e] = 0.0f;
+#pragma unroll
+  for (int c = 0; c < 8; ++c) {
+    s[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8bf, ka[c]), q[c], s[0], 0, 0, 0);
+    ka[c] = kt[(r + 32) * 16 + ((2 * c + hf) ^ (r & 15))];
+  }
+#pragma unroll
+  for (int c = 0; c < 8; ++c)
+    s[1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8bf, ka[c]), q[c], s[1], 0, 0, 0);
+  // eight reads in flight, then one behind each product of the first half
+  __builtin_amdgcn_sched_group_barrier(0x100, 8, 0);
+#pragma unroll
+  for (int c = 0; c < 8; ++c) {
+    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+    __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+  }
+  __builtin_amdgcn_sched_group_barrier(0x008, 8, 0);
+}
+
+// A operand of step (o, d) of O^T = V^T P^T: lane (channel 32 d + lane % 32,
+// half hf) holds keys 16 o + 8 hf .. + 7 of its channel: two transposing reads,
+// each of which gives the 16 lanes of a group one column of the 4 x 16 block
+// whose rows 4 lanes each point at.  `lane_v` is the lane's part of the address
+// (bytes), without the chunk bits of d.
+__device__ __forceinline__ int lane_v(int lane) {
+  const int i = lane & 15, row = ((lane >> 5) << 3) + (i >> 2);
+  const int chunk = (((lane >> 4) & 1) << 1) + ((i >> 1) & 1);
+  return row * 256 + ((chunk ^ ((i >> 2) << 2)) << 4) + ((i & 1) << 3);
+}
+__device__ __forceinline__ v8bf read_v(const v4u* vt, int lane_part, int o, int d) {
+  typedef short v4s __attribute__((ext_vector_type(4)));
+  typedef short v8s __attribute__((ext_vector_type(8)));
+  const char* base = reinterpret_cast<const char*>(vt);
+  v4s x[2];
+#pragma unroll
+  for (int u = 0; u < 2; ++u) {   // keys + 4 u
+    const char* p = base + ((lane_part ^ (d << 6)) + (o * 16 + u * 4) * 256);
+    x[u] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+        (__attribute__((address_space(3))) v4s*)reinterpret_cast<const v4s*>(p));
+  }
+  const v8s r = {x[0][0], x[0][1], x[0][2], x[0][3], x[1][0], x[1][1], x[1][2], x[1][3]};
+  return __builtin_bit_cast(v8bf, r);
+}
+
+// Workgroup (b, t, sp, j) of NW waves: rows [32 NW t, 32 NW (t + 1)) of a
+// sequence's rows for KV head j, share sp of the keys they see.  One barrier a tile: iteration c
+// takes the scores of tile c, then the weights of tile c step by step between
+// the products of V with the weights of tile c - 1, so that exponentials and
+// matrix cores run side by side.  K is staged a tile ahead, V in time, the
+// loads of both a tile earlier still.
+//
+// The reference of a row's weights is the maximum of the first tile it sees;
+// later tiles need no maximum of their own: bf16 weights keep their precision
+// at any size, so the reference moves only when a lane's weights of a tile sum
+// to more than 2^60.
+constexpr float kFarSum = 0x1p60f;
+
+template <int FMT, int NW>
+__global__ void __launch_bounds__(NW * 64, NW / 4)
+paged_many_kernel(AttnArgs a, const int32_t* __restrict__ table, int tiles) {
+  constexpr int kRowTile = NW * 32, U = 16 / NW;
+  __shared__ ManyLds lds;
   const int j = blockIdx.x % a.g.Hkv;
   int id = blockIdx.x / a.g.Hkv;
   const int sp = id % a.S_many;
@@ -508,56 +571,96 @@ paged_many_kernel(AttnArgs a, int tiles) {
     for (int e = 0; e < 16; ++e) acc[d][e] = 0.0f;
   float m = kFloor, l = 0.0f;
 
-  const bool is_v = threadIdx.x < 128;
-  const int st = threadIdx.x & 127;
-  const int kg = is_v ? st & 7 : st >> 4, chunk = is_v ? st >> 3 : st & 15;
-  Stage<FMT> g;
   if (first < end) {
-    stage_load<FMT>(g, a, page_of(a.g, b, first * kKeyTile + kg * 8), j, first, kg, chunk, is_v);
-    stage_store<FMT>(g, lds[first & 1], first, sq.n_kv, kg, chunk, is_v);
-    int page = page_of(a.g, b, min(first + 1, end - 1) * kKeyTile + kg * 8);
+    const int kg = threadIdx.x >> 4, chunk = threadIdx.x & 15;
+    // the wave's rows of a tile (4 U, aligned) lie in one page: a scalar lookup
+    // an iteration ahead of its use, looked at when it is used
+    auto entry_of = [&](int tile) {
+      return __builtin_amdgcn_readfirstlane((min(tile, end - 1) * kKeyTile + w * (4 * U)) >> a.g.page_log2);
+    };
+    auto entry_at = [&](int tile) { return table[(size_t)b * a.g.max_pages + min(entry_of(tile), a.g.max_pages - 1)]; };
+    auto page_at = [&](int tile, int entry) {
+      return entry_of(tile) < a.g.max_pages && (unsigned)entry < (unsigned)a.g.n_pages ? entry : -1;
+    };
+    auto tile_at = [&](int tile) { return min(tile, end - 1); };
+    // of the keys of accumulators 4 f .. 4 f + 3 of half x: what takes a score to
+    // log2 units, and the scale of the value row
+    auto four = [&](const float* p, int x, int f) {
+      return *reinterpret_cast<const v4f*>(p + x * 32 + (f >> 1) * 16 + hf * 8 + (f & 1) * 4);
+    };
+    auto factor = [&](int buf, int x, int f) {
+      if constexpr (FMT == kBf16) return v4f{a.c_log2, a.c_log2, a.c_log2, a.c_log2};
+      else return four(lds.ks[buf], x, f);
+    };
+    auto value_scale = [&](int buf, int x, int f) {
+      if constexpr (FMT == kBf16) return v4f{1.0f, 1.0f, 1.0f, 1.0f};
+      else return four(lds.vs[buf], x, f);
+    };
+    Stage<FMT, U> gk, gv;
+    int pk = page_at(first, entry_at(first));
+    stage_load<FMT, true, U>(gk, a, pk, j, first, kg, chunk);
+    stage_load<FMT, false, U>(gv, a, pk, j, first, kg, chunk);
+    store_k<FMT, U>(gk, lds, first & 1, first, sq.n_kv, kg, chunk, a.c_log2);
+    pk = page_at(first + 1, entry_at(first + 1));
+    stage_load<FMT, true, U>(gk, a, pk, j, tile_at(first + 1), kg, chunk);
+    int next = entry_at(first + 2);   // table entry of the tile after the next
+    v8bf pprev[4];
+#pragma unroll
+    for (int o = 0; o < 4; ++o) pprev[o] = v8bf{};
+    // zeros where the first iteration multiplies V of "tile first - 1"
+#pragma unroll
+    for (int x = 0; x < U; ++x) lds.v[(first + 1) & 1][threadIdx.x + x * NW * 64] = v4u{0u, 0u, 0u, 0u};
+    const int lv = lane_v(lane);
     for (int tile = first; tile < end; ++tile) {
-      if (tile + 1 < end) stage_load<FMT>(g, a, page, j, tile + 1, kg, chunk, is_v);
-      page = page_of(a.g, b, min(tile + 2, end - 1) * kKeyTile + kg * 8);
+      const int kb = tile & 1, vb = kb ^ 1;
       __syncthreads();
-      const ManyLds& T = lds[tile & 1];
       v16f s[2];
-#pragma unroll
-      for (int x = 0; x < 2; ++x) {
-#pragma unroll
-        for (int e = 0; e < 16; ++e) s[x][e] = 0.0f;
-        const int r = x * 32 + many_key(n);
-#pragma unroll
-        for (int c = 0; c < 8; ++c) {
-          const v4u ka = reinterpret_cast<const v4u*>(T.k)[r * 16 + ((2 * c + hf) ^ (r & 15))];
-          s[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8bf, ka), q[c], s[x], 0, 0, 0);
-        }
-      }
-      if constexpr (FMT != kBf16) {
-#pragma unroll
-        for (int x = 0; x < 2; ++x)
-#pragma unroll
-          for (int e = 0; e < 16; ++e) s[x][e] *= T.ks[x * 32 + (e >> 3) * 16 + hf * 8 + (e & 7)];
-      }
-      const uint64_t gone = *reinterpret_cast<const uint64_t*>(T.gone);
-      if (gone != 0 || (tile + 1) * kKeyTile > n_all) {
+      many_scores(s, lds.k[kb], q, n, hf);
+      // K of the next tile (past the end the last one again: no branch); its
+      // buffer was last read before the barrier
+      store_k<FMT, U>(gk, lds, kb ^ 1, tile_at(tile + 1), sq.n_kv, kg, chunk, a.c_log2);
+      const int pn = page_at(tile + 2, next);
+      next = entry_at(tile + 3);
+      stage_load<FMT, true, U>(gk, a, pn, j, tile_at(tile + 2), kg, chunk);
+      const uint64_t* gp = reinterpret_cast<const uint64_t*>(lds.gone[kb]);
+      const uint64_t g0 = gp[0], g1 = gp[1];
+      if ((g0 | g1) != 0 || (tile + 1) * kKeyTile > n_all) {
 #pragma unroll
         for (int x = 0; x < 2; ++x)
 #pragma unroll
           for (int e = 0; e < 16; ++e) {
-            const int grp = x * 4 + (e >> 3) * 2 + hf, key = tile * kKeyTile + grp * 8 + (e & 7);
-            const bool hid = key > last || ((gone >> (8 * grp)) & 1);
+            const int grp = (e >> 3) * 4 + hf * 2 + ((e >> 2) & 1), key = tile * kKeyTile + x * 32 + grp * 4 + (e & 3);
+            const bool hid = key > last || (((x ? g1 : g0) >> (8 * grp)) & 1);
             s[x][e] = hid ? -INFINITY : s[x][e];
           }
       }
-      float top = s[0][0];
+      v8bf pcur[4];
+      float ps = 0.0f;
+      __builtin_amdgcn_s_setprio(1);
 #pragma unroll
-      for (int x = 0; x < 2; ++x)
+      for (int u = 0; u < 16; ++u) {
+        const int d = u & 3, o = u >> 2;
+        acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(read_v(lds.v[vb], lv, o, d), pprev[o], acc[d], 0, 0, 0);
+        const int x = u >> 3, e = (u & 7) * 2;
+        const v4f f = factor(kb, x, e >> 2);
+        const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[x][e], f[e & 3], -m));
+        const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[x][e + 1], f[(e & 3) + 1], -m));
+        ps += p0 + p1;
+        const v4f vs = value_scale(kb, x, e >> 2);
+        pcur[x * 2 + (e >> 3)][e & 7] = (__bf16)(p0 * vs[e & 3]);
+        pcur[x * 2 + (e >> 3)][(e & 7) + 1] = (__bf16)(p1 * vs[(e & 3) + 1]);
+      }
+      // the weights stay here, beside the products
+      asm volatile("" : "+v"(pcur[0]), "+v"(pcur[1]), "+v"(pcur[2]), "+v"(pcur[3]), "+v"(ps));
+      __builtin_amdgcn_s_setprio(0);
+      if (tile == first || __ballot(!(ps <= kFarSum))) {
+        float top = -INFINITY;
 #pragma unroll
-        for (int e = 0; e < 16; ++e) top = fmaxf(top, s[x][e]);
-      top = fmaxf(top, __shfl_xor(top, 32, 64)) * a.c_log2;
-      const float mnew = top > m + kLazy ? top : m;
-      if (__ballot(mnew != m)) {
+        for (int x = 0; x < 2; ++x)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) top = fmaxf(top, s[x][e] * factor(kb, x, e >> 2)[e & 3]);
+        top = fmaxf(top, __shfl_xor(top, 32, 64));
+        const float mnew = fmaxf(m, top);
         const float f = __builtin_amdgcn_exp2f(m - mnew);
 #pragma unroll
         for (int d = 0; d < 4; ++d)
@@ -565,28 +668,30 @@ paged_many_kernel(AttnArgs a, int tiles) {
           for (int e = 0; e < 16; ++e) acc[d][e] *= f;
         l *= f;
         m = mnew;
+        ps = 0.0f;
+#pragma unroll
+        for (int x = 0; x < 2; ++x)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            const float pw = __builtin_amdgcn_exp2f(__builtin_fmaf(s[x][e], factor(kb, x, e >> 2)[e & 3], -m));
+            ps += pw;
+            pcur[x * 2 + (e >> 3)][e & 7] = (__bf16)(pw * value_scale(kb, x, e >> 2)[e & 3]);
+          }
       }
+      l += ps;
+      // V of this tile: its buffer was last read before the barrier too
+      store_v<FMT, U>(gv, lds, kb, tile, sq.n_kv, kg, chunk);
+      stage_load<FMT, false, U>(gv, a, pk, j, tile_at(tile + 1), kg, chunk);
+      pk = pn;
 #pragma unroll
-      for (int x = 0; x < 2; ++x)
+      for (int o = 0; o < 4; ++o) pprev[o] = pcur[o];
+    }
+    __syncthreads();
 #pragma unroll
-        for (int o = 0; o < 2; ++o) {
-          v8bf p;
-#pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            float pw = __builtin_amdgcn_exp2f(__builtin_fmaf(s[x][o * 8 + e], a.c_log2, -m));
-            l += pw;
-            if constexpr (FMT != kBf16) pw *= T.vs[x * 32 + o * 16 + hf * 8 + e];
-            p[e] = (__bf16)pw;
-          }
-          const int ck = x * 4 + o * 2 + hf;
-#pragma unroll
-          for (int d = 0; d < 4; ++d) {
-            const int ch = d * 32 + n;
-            const v4u va = reinterpret_cast<const v4u*>(T.v)[ch * 8 + (ck ^ ((ch >> 1) & 7))];
-            acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8bf, va), p, acc[d], 0, 0, 0);
-          }
-        }
-      if (tile + 1 < end) stage_store<FMT>(g, lds[(tile + 1) & 1], tile + 1, sq.n_kv, kg, chunk, is_v);
+    for (int u = 0; u < 16; ++u) {
+      const int d = u & 3, o = u >> 2;
+      acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(read_v(lds.v[(end + 1) & 1], lv, o, d), pprev[o], acc[d],
+                                                       0, 0, 0);
     }
   }
   l += __shfl_xor(l, 32, 64);
@@ -779,7 +884,7 @@ paged_many_mass_kernel(AttnArgs a) {
   v4u g0, g1;
   float2 gs;
   auto load = [&](int tile) {
-    const int r = tile * 32 + sr, rr = min(r, rows - 1), i = rr / a.g.g;
+    const int r = tile * 32 + sr, rr = min(r, rows - 1), i = token_of(a, rr);
     const size_t qrow = (size_t)(sq.t0 + i) * a.g.Hq + (size_t)j * a.g.g + (rr - i * a.g.g);
     const v4u* src = reinterpret_cast<const v4u*>(a.q + qrow * kHeadDim);
     g0 = src[sc];
@@ -811,8 +916,8 @@ paged_many_mass_kernel(AttnArgs a) {
     }
     const float2 ml = ss[buf][n];
     // the tile's first token sees every key of the wave?
-    const bool cut = key0 + KW * 32 > min(sq.len + tile * 32 / a.g.g + 1, sq.n_kv);
-    const int last = cut ? min(sq.len + min(tile * 32 + n, rows - 1) / a.g.g, sq.n_kv - 1) : 0x7fffffff;
+    const bool cut = key0 + KW * 32 > min(sq.len + token_of(a, tile * 32) + 1, sq.n_kv);
+    const int last = cut ? min(sq.len + token_of(a, min(tile * 32 + n, rows - 1)), sq.n_kv - 1) : 0x7fffffff;
 #pragma unroll
     for (int x = 0; x < KW; ++x)
 #pragma unroll
@@ -848,7 +953,8 @@ struct Plan {
   int few_max;
   int S_few, S_many;
   bool join_few, join_many;
-  int row_tiles;       // row tiles of a sequence in the many-row kernel
+  int waves;           // of a workgroup of the many-row kernel (32 rows each)
+  int row_tiles;       // row tiles of a sequence there
   int64_t n_kv;        // bound on a sequence's slots
   int logit_stride;
   size_t part, logit, stat;   // workspace bytes
@@ -871,9 +977,10 @@ Plan plan_of(const hyq_pcache& c, const hyq_pbatch& b, int mass) {
   const int64_t units = std::max<int64_t>(1, (p.n_kv + kUnit - 1) / kUnit);
   const int64_t ktiles = std::max<int64_t>(1, (p.n_kv + kKeyTile - 1) / kKeyTile);
   p.S_few = (int)std::max<int64_t>(1, std::min({(512 + heads - 1) / heads, (units + 7) / 8, (int64_t)64}));
-  p.row_tiles = (rows + kRowTile - 1) / kRowTile;
+  p.waves = rows <= 128 ? 4 : 8;
+  p.row_tiles = (rows + p.waves * 32 - 1) / (p.waves * 32);
   const int64_t wg = heads * p.row_tiles;
-  p.S_many = (int)std::max<int64_t>(1, std::min({512 / wg, (ktiles + 7) / 8, (int64_t)64}));
+  p.S_many = (int)std::max<int64_t>(1, std::min({256 / wg, (ktiles + 7) / 8, (int64_t)64}));
   p.join_few = p.few && (p.S_few > 1 || mass);
   p.join_many = p.many && p.S_many > 1;
   const int S = std::max(p.join_few ? p.S_few : 0, p.join_many ? p.S_many : 0);
@@ -893,8 +1000,11 @@ template <int FMT>
 hipError_t launch(const Plan& p, const AttnArgs& a, hipStream_t st) {
   const unsigned heads = (unsigned)(a.g.B * a.g.Hkv);
   if (p.few) paged_few_kernel<FMT><<<heads * p.S_few, kFewThreads, 0, st>>>(a);
-  if (p.many)
-    paged_many_kernel<FMT><<<heads * p.row_tiles * p.S_many, kManyThreads, 0, st>>>(a, p.row_tiles);
+  if (p.many) {
+    const unsigned wg = heads * p.row_tiles * p.S_many;
+    if (p.waves == 4) paged_many_kernel<FMT, 4><<<wg, 256, 0, st>>>(a, a.g.table, p.row_tiles);
+    else paged_many_kernel<FMT, 8><<<wg, 512, 0, st>>>(a, a.g.table, p.row_tiles);
+  }
   const bool mass = a.mass_mode != HYQ_MASS_NONE;
   if (p.join_few) {
     const unsigned keys = mass ? (unsigned)((p.n_kv + kMassKeys - 1) / kMassKeys) : 0u;
@@ -931,6 +1041,7 @@ hipError_t launch_paged_attn(const hyq_pcache& c, const hyq_pbatch& b, const uin
   a.out = out;
   a.out_bf16 = out_dtype;
   a.mass_mode = mass;
+  a.inv_g = (uint32_t)((((uint64_t)1 << 32) + a.g.g - 1) / a.g.g);
   a.c_log2 = softmax_scale * 1.44269504088896340736f;
   a.few_max = p.few_max;
   a.S_few = p.S_few;
