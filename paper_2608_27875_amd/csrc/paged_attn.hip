@@ -535,7 +535,7 @@ __device__ __forceinline__ v8bf read_v(const v4u* vt, int lane_part, int o, int 
 constexpr float kFarSum = 0x1p60f;
 
 template <int FMT, int NW>
-__global__ void __launch_bounds__(NW * 64, NW / 4)
+__global__ void __launch_bounds__(NW * 64, 2)
 paged_many_kernel(AttnArgs a, const int32_t* __restrict__ table, int tiles) {
   constexpr int kRowTile = NW * 32, U = 16 / NW;
   __shared__ ManyLds lds;
@@ -635,7 +635,7 @@ paged_many_kernel(AttnArgs a, const int32_t* __restrict__ table, int tiles) {
           }
       }
       v8bf pcur[4];
-      float ps = 0.0f;
+      float ps = 0.0f, ps1 = 0.0f;
       __builtin_amdgcn_s_setprio(1);
 #pragma unroll
       for (int u = 0; u < 16; ++u) {
@@ -645,13 +645,15 @@ paged_many_kernel(AttnArgs a, const int32_t* __restrict__ table, int tiles) {
         const v4f f = factor(kb, x, e >> 2);
         const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[x][e], f[e & 3], -m));
         const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[x][e + 1], f[(e & 3) + 1], -m));
-        ps += p0 + p1;
+        ps += p0;
+        ps1 += p1;
         const v4f vs = value_scale(kb, x, e >> 2);
         pcur[x * 2 + (e >> 3)][e & 7] = (__bf16)(p0 * vs[e & 3]);
         pcur[x * 2 + (e >> 3)][(e & 7) + 1] = (__bf16)(p1 * vs[(e & 3) + 1]);
       }
       // the weights stay here, beside the products
-      asm volatile("" : "+v"(pcur[0]), "+v"(pcur[1]), "+v"(pcur[2]), "+v"(pcur[3]), "+v"(ps));
+      asm volatile("" : "+v"(pcur[0]), "+v"(pcur[1]), "+v"(pcur[2]), "+v"(pcur[3]), "+v"(ps), "+v"(ps1));
+      ps += ps1;
       __builtin_amdgcn_s_setprio(0);
       if (tile == first || __ballot(!(ps <= kFarSum))) {
         float top = -INFINITY;
@@ -841,107 +843,109 @@ paged_few_finish_kernel(AttnArgs a) {
 }
 
 // Many rows: the products again, now that every row's maximum and sum are
-// known.  A wave owns KW * 32 keys (their K rows stay in registers); the
-// workgroup walks the rows that see any of its keys in tiles of 32, staged in
-// LDS for its four waves (chunk c of row r at c ^ (r & 15)), the next tile's
-// loads in flight.
-constexpr int kMassThreads = 256;
+// known.  A wave owns 32 keys (their K rows stay in registers); the workgroup
+// walks the rows that see any of its 128 keys in tiles of 64, staged in LDS for
+// its four waves (chunk c of row r at c ^ (r & 15)), the next tile's loads in
+// flight.
+constexpr int kMassThreads = 256, kMassTile = 64;
 
-template <int FMT, int KW>
-__global__ void __launch_bounds__(kMassThreads, KW == 2 ? 2 : 3)
+template <int FMT>
+__global__ void __launch_bounds__(kMassThreads, FMT == kBf16 ? 3 : 2)
 paged_many_mass_kernel(AttnArgs a) {
-  __shared__ v4u qs[2][32 * 16];
-  __shared__ float2 ss[2][32];
+  __shared__ v4u qs[2][kMassTile * 16];
+  __shared__ float2 ss[2][kMassTile];
   const int j = blockIdx.x % a.g.Hkv, b = blockIdx.x / a.g.Hkv;
   const Seq sq = seq_of(a.g, b);
   const int rows = sq.n_new * a.g.g;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int lane = threadIdx.x & 63, n = lane & 31, hf = lane >> 5;
-  const int wg_key = blockIdx.y * (4 * KW * 32), key0 = wg_key + w * (KW * 32);
+  const int wg_key = blockIdx.y * 128, key0 = wg_key + w * 32;
   if (rows <= a.few_max || wg_key >= sq.n_kv) return;
-  v8bf kf[KW][8];
-  float kse[KW][16], sum[KW][16];
-#pragma unroll
-  for (int x = 0; x < KW; ++x) {
-    const int key = key0 + x * 32 + n, p = page_of(a.g, b, key);
+  v8bf kf[8];
+  float kse[16], sum[16];   // of key 8 (e / 4) + 4 hf + e % 4: what takes its scores to log2 units; its mass
+  {
+    const int key = key0 + n, p = page_of(a.g, b, key);
     const size_t row = pool_row(a.g, max(p, 0), j, key);
     const uint8_t* src = a.k + row * row_bytes<FMT>();
 #pragma unroll
     for (int c = 0; c < 8; ++c)
-      kf[x][c] = __builtin_bit_cast(v8bf, to_bf16<FMT>(*reinterpret_cast<const typename Eight<FMT>::type*>(
-                                              src + (2 * c + hf) * (row_bytes<FMT>() / 16))));
+      kf[c] = __builtin_bit_cast(v8bf, to_bf16<FMT>(*reinterpret_cast<const typename Eight<FMT>::type*>(
+                                           src + (2 * c + hf) * (row_bytes<FMT>() / 16))));
     float ks = 1.0f;
-    if constexpr (FMT != kBf16) ks = a.ks[row];
+    if constexpr (FMT != kBf16) ks = fmaxf(a.ks[row], 1e-30f);   // hidden scores stay -inf
 #pragma unroll
     for (int e = 0; e < 16; ++e) {
-      kse[x][e] = FMT == kBf16 ? a.c_log2 : __shfl(ks, 8 * (e >> 2) + 4 * hf + (e & 3), 64) * a.c_log2;
-      sum[x][e] = 0.0f;
+      kse[e] = FMT == kBf16 ? a.c_log2 : __shfl(ks, 8 * (e >> 2) + 4 * hf + (e & 3), 64) * a.c_log2;
+      sum[e] = 0.0f;
     }
   }
   // rows that see the first of the workgroup's keys: from token wg_key - len on
-  const int first = max(0, wg_key - sq.len) * a.g.g / 32, end = (rows + 31) / 32;
-  const int sr = threadIdx.x >> 3, sc = (threadIdx.x & 7) * 2;   // the row and chunks this thread stages
-  v4u g0, g1;
+  const int first = max(0, wg_key - sq.len) * a.g.g / kMassTile, end = (rows + kMassTile - 1) / kMassTile;
+  const int sr = threadIdx.x >> 2, sc = (threadIdx.x & 3) * 4;   // the row and chunks this thread stages
+  const uint16_t* const qh = a.q + ((size_t)sq.t0 * a.g.Hq + (size_t)j * a.g.g) * kHeadDim + sc * 8;
+  const float2* const sh = a.stat + (size_t)sq.t0 * a.g.Hq + (size_t)j * a.g.g;
+  v4u g[4];
   float2 gs;
   auto load = [&](int tile) {
-    const int r = tile * 32 + sr, rr = min(r, rows - 1), i = token_of(a, rr);
-    const size_t qrow = (size_t)(sq.t0 + i) * a.g.Hq + (size_t)j * a.g.g + (rr - i * a.g.g);
-    const v4u* src = reinterpret_cast<const v4u*>(a.q + qrow * kHeadDim);
-    g0 = src[sc];
-    g1 = src[sc + 1];
-    gs = a.stat[qrow];
+    const int r = tile * kMassTile + sr, rr = min(r, rows - 1), i = token_of(a, rr);
+    const size_t at = (size_t)i * a.g.Hq + (rr - i * a.g.g);
+#pragma unroll
+    for (int x = 0; x < 4; ++x) g[x] = reinterpret_cast<const v4u*>(qh + at * kHeadDim)[x];
+    gs = sh[at];
     if (r >= rows) gs.y = 0.0f;
   };
   auto store = [&](int buf) {
-    qs[buf][sr * 16 + (sc ^ (sr & 15))] = g0;
-    qs[buf][sr * 16 + ((sc + 1) ^ (sr & 15))] = g1;
+#pragma unroll
+    for (int x = 0; x < 4; ++x) qs[buf][sr * 16 + ((sc + x) ^ (sr & 15))] = g[x];
     if (sc == 0) ss[buf][sr] = gs;
   };
   load(first);
   store(first & 1);
   for (int tile = first; tile < end; ++tile) {
-    if (tile + 1 < end) load(tile + 1);
+    load(min(tile + 1, end - 1));
     __syncthreads();
     const int buf = tile & 1;
-    v16f s[KW];
 #pragma unroll
-    for (int x = 0; x < KW; ++x)
+    for (int u = 0; u < 2; ++u) {
+      v16f s;
 #pragma unroll
-      for (int e = 0; e < 16; ++e) s[x][e] = 0.0f;
+      for (int e = 0; e < 16; ++e) s[e] = 0.0f;
+      v4u q[8];
 #pragma unroll
-    for (int c = 0; c < 8; ++c) {
-      const v8bf q = __builtin_bit_cast(v8bf, qs[buf][n * 16 + ((2 * c + hf) ^ (n & 15))]);
+      for (int c = 0; c < 8; ++c) q[c] = qs[buf][(u * 32 + n) * 16 + ((2 * c + hf) ^ (n & 15))];
+      const float2 ml = ss[buf][u * 32 + n];
 #pragma unroll
-      for (int x = 0; x < KW; ++x) s[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[x][c], q, s[x], 0, 0, 0);
-    }
-    const float2 ml = ss[buf][n];
-    // the tile's first token sees every key of the wave?
-    const bool cut = key0 + KW * 32 > min(sq.len + token_of(a, tile * 32) + 1, sq.n_kv);
-    const int last = cut ? min(sq.len + token_of(a, min(tile * 32 + n, rows - 1)), sq.n_kv - 1) : 0x7fffffff;
+      for (int c = 0; c < 8; ++c)
+        s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[c], __builtin_bit_cast(v8bf, q[c]), s, 0, 0, 0);
+      // all reads in flight before the first product
+      __builtin_amdgcn_sched_group_barrier(0x100, 9, 0);
+      __builtin_amdgcn_sched_group_barrier(0x008, 8, 0);
+      // some row of these 32 does not see some key of the wave
+      const int r0 = tile * kMassTile + u * 32;
+      if (key0 + 32 > min(sq.len + token_of(a, min(r0, rows - 1)) + 1, sq.n_kv)) {
+        const int last = min(sq.len + token_of(a, min(r0 + n, rows - 1)), sq.n_kv - 1);
 #pragma unroll
-    for (int x = 0; x < KW; ++x)
-#pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        float z = s[x][e];
-        if (cut) z = key0 + x * 32 + 8 * (e >> 2) + 4 * hf + (e & 3) <= last ? z : -INFINITY;
-        sum[x][e] = __builtin_fmaf(__builtin_amdgcn_exp2f(__builtin_fmaf(z, kse[x][e], -ml.x)), ml.y, sum[x][e]);
+        for (int e = 0; e < 16; ++e)
+          s[e] = key0 + 8 * (e >> 2) + 4 * hf + (e & 3) <= last ? s[e] : -INFINITY;
       }
-    if (tile + 1 < end) store((tile + 1) & 1);
+#pragma unroll
+      for (int e = 0; e < 16; ++e)
+        sum[e] = __builtin_fmaf(__builtin_amdgcn_exp2f(__builtin_fmaf(s[e], kse[e], -ml.x)), ml.y, sum[e]);
+    }
+    store((tile + 1) & 1);
   }
 #pragma unroll
-  for (int x = 0; x < KW; ++x)
+  for (int e = 0; e < 16; ++e) {
+    float v = sum[e];
 #pragma unroll
-    for (int e = 0; e < 16; ++e) {
-      float v = sum[x][e];
-#pragma unroll
-      for (int o = 16; o >= 1; o >>= 1) v += __shfl_xor(v, o, 64);
-      const int key = key0 + x * 32 + 8 * (e >> 2) + 4 * hf + (e & 3);
-      if (n != 0 || key >= sq.n_kv) continue;
-      const int p = page_of(a.g, b, key);
-      if (p < 0) continue;
-      float* m = a.mass + pool_row(a.g, p, j, key);
-      *m = a.mass_mode == HYQ_MASS_ADD ? *m + v : v;
-    }
+    for (int o = 16; o >= 1; o >>= 1) v += __shfl_xor(v, o, 64);
+    const int key = key0 + 8 * (e >> 2) + 4 * hf + (e & 3);
+    if (n != 0 || key >= sq.n_kv) continue;
+    const int p = page_of(a.g, b, key);
+    if (p < 0) continue;
+    float* m = a.mass + pool_row(a.g, p, j, key);
+    *m = a.mass_mode == HYQ_MASS_ADD ? *m + v : v;
+  }
 }
 
 // ---------------------------------------------------------------------------
@@ -960,8 +964,6 @@ struct Plan {
   size_t part, logit, stat;   // workspace bytes
   size_t total() const { return part + logit + stat; }
 };
-
-constexpr int kMassWide = 256;   // workgroups from which a wave of the masses owns 64 keys
 
 size_t up256(size_t x) { return (x + 255) & ~(size_t)255; }
 
@@ -1011,12 +1013,8 @@ hipError_t launch(const Plan& p, const AttnArgs& a, hipStream_t st) {
     paged_few_finish_kernel<<<dim3(heads, kFewRows + keys), kJoinThreads, 0, st>>>(a);
   }
   if (p.join_many) paged_join_kernel<<<(unsigned)(a.g.T * a.g.Hq), kJoinThreads, 0, st>>>(a);
-  if (p.many && mass) {
-    if ((int64_t)heads * ((p.n_kv + 255) / 256) >= kMassWide)
-      paged_many_mass_kernel<FMT, 2><<<dim3(heads, (unsigned)((p.n_kv + 255) / 256)), kMassThreads, 0, st>>>(a);
-    else
-      paged_many_mass_kernel<FMT, 1><<<dim3(heads, (unsigned)((p.n_kv + 127) / 128)), kMassThreads, 0, st>>>(a);
-  }
+  if (p.many && mass)
+    paged_many_mass_kernel<FMT><<<dim3(heads, (unsigned)((p.n_kv + 127) / 128)), kMassThreads, 0, st>>>(a);
   return hipGetLastError();
 }
 
