@@ -979,10 +979,10 @@ Plan plan_of(const hyq_pcache& c, const hyq_pbatch& b, int mass) {
   const int64_t units = std::max<int64_t>(1, (p.n_kv + kUnit - 1) / kUnit);
   const int64_t ktiles = std::max<int64_t>(1, (p.n_kv + kKeyTile - 1) / kKeyTile);
   p.S_few = (int)std::max<int64_t>(1, std::min({(512 + heads - 1) / heads, (units + 7) / 8, (int64_t)64}));
-  p.waves = rows <= 128 ? 4 : 8;
+  p.waves = rows <= 128 || p.n_kv < 4096 ? 4 : 8;
   p.row_tiles = (rows + p.waves * 32 - 1) / (p.waves * 32);
   const int64_t wg = heads * p.row_tiles;
-  p.S_many = (int)std::max<int64_t>(1, std::min({256 / wg, (ktiles + 7) / 8, (int64_t)64}));
+  p.S_many = (int)std::max<int64_t>(1, std::min({(p.waves == 4 ? 512 : 256) / wg, (ktiles + 7) / 8, (int64_t)64}));
   p.join_few = p.few && (p.S_few > 1 || mass);
   p.join_many = p.many && p.S_many > 1;
   const int S = std::max(p.join_few ? p.S_few : 0, p.join_many ? p.S_many : 0);
