@@ -513,8 +513,9 @@ HYQ_API int hyq_paged_ws_bytes(const hyq_pcache* cache, const hyq_pbatch* batch,
  * Precision: bf16 products (8-bit codes are exact in bf16, their scales are
  * applied in float32), float32 sums; the weights enter the products with V as
  * a high + low bf16 pair where a sequence has at most 16 query rows per KV
- * head (new tokens * Hq/Hkv), and as bf16 where it has more.  Every result is
- * the same from run to run: nothing is added atomically.
+ * head (new tokens * Hq/Hkv; of a single sequence, max_new * Hq/Hkv), and as
+ * bf16 where it has more.  Every result is the same from run to run: nothing
+ * is added atomically.
  * Allocates nothing and keeps no state; it can be captured in a HIP graph
  * (lens, tables and token counts may change between replays, within the
  * bounds).  ws: scratch of hyq_paged_ws_bytes; calls that overlap need one each.

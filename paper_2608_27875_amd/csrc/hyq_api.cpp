@@ -308,7 +308,7 @@ int check_pcache(const hyq_pcache* c) {
 }
 
 // Bounds of a batch (its device arrays are checked by the calls that read them).
-constexpr int64_t kMaxSlots = (int64_t)1 << 23;   // of one sequence
+constexpr int64_t kMaxSlots = (int64_t)1 << 22;   // of one sequence
 constexpr int64_t kMaxRows = (int64_t)1 << 24;    // query rows (tokens * heads) of one step
 int check_pbatch(const hyq_pcache* c, const hyq_pbatch* b) {
   if (!b) return fail(HYQ_EINVAL, "batch is NULL");
@@ -322,6 +322,9 @@ int check_pbatch(const hyq_pcache* c, const hyq_pbatch* b) {
     return fail(HYQ_EUNSUPPORTED, "%d token rows in one step not supported", b->T);
   if ((int64_t)b->B * c->Hkv > 32768)
     return fail(HYQ_EUNSUPPORTED, "%d sequences in one step not supported", b->B);
+  if (!hyq::paged_grid_fits(*c, *b))
+    return fail(HYQ_EUNSUPPORTED, "%d sequences of up to %d new tokens in one step not supported", b->B,
+                b->max_new);
   return HYQ_OK;
 }
 

@@ -101,6 +101,8 @@ hipError_t launch_norm_rope(const hyq_shape& s, const hyq_rope& r, const RopeRow
                             uint16_t* K, uint16_t* V, hipStream_t st);
 hipError_t launch_paged_append(const hyq_pcache& c, const hyq_pbatch& b, const hyq_rope& r,
                                const RopeRows& x, uint16_t* q_out, hipStream_t st);
+// Whether the workgroups that the batch's bounds ask for fit a grid.
+bool paged_grid_fits(const hyq_pcache& c, const hyq_pbatch& b);
 size_t paged_ws_bytes(const hyq_pcache& c, const hyq_pbatch& b, int mass);
 hipError_t launch_paged_attn(const hyq_pcache& c, const hyq_pbatch& b, const uint16_t* q,
                              float softmax_scale, int mass, void* out, int out_dtype, void* ws,

@@ -13,8 +13,8 @@
 //   32 keys, S^T = K q^T in 16x16x32 products with the keys as rows; the
 //   accumulators are then the B operand of O^T = V^T P^T, whose A operand is
 //   eight rows of V transposed in registers (one byte permute per pair).
-//   many rows (chunks): bound by the matrix cores.  Workgroups of 128 rows
-//   stage tiles of 64 keys in LDS, V transposed on the way.
+//   many rows (chunks): bound by the matrix cores.  Workgroups of 128 or 256
+//   rows stage tiles of 64 keys in LDS; V is read from there transposed.
 //
 // Keys are split over workgroups where there are too few rows to fill the
 // chip; partial sums (acc, max, sum) then go through a workspace and a second
@@ -56,14 +56,14 @@ struct AttnArgs {
   int S_few, S_many;   // splits of the keys in the two kernels
   int join_few;        // whether the few-row kernel leaves partials
   float* part;         // [S][T][Hq][kPart]
-  float* logit;        // few rows with mass: [B][Hkv][kFewRows][logit_stride]
-  int logit_stride;
+  float* logit;        // few rows with mass: [B][Hkv][logit_rows][logit_stride]
+  int logit_rows, logit_stride;
   uint32_t inv_g;      // ceil(2^32 / g) (g > 1): r / g for the rows of a step
   float2* stat;        // many rows with mass: (max, 1 / sum) of every query row [T][Hq]
 };
 
-// Token of row r of a KV head's rows: r / g.  Exact for r < 2^29 (the product
-// is off by less than r g / 2^32 < 1 / g, g <= 8).
+// Token of row r of a KV head's rows: r / g.  Exact for r < 2^29 (the quotient
+// is too large by less than r / 2^32 < 1 / g, g <= 8).
 __device__ __forceinline__ int token_of(const AttnArgs& a, int r) {
   return a.g.g == 1 ? r : (int)__umulhi((uint32_t)r, a.inv_g);
 }
@@ -323,7 +323,7 @@ paged_few_kernel(AttnArgs a) {
   const int nu = (sq.n_kv + kUnit - 1) / kUnit, nw = a.S_few * kFewWaves, gw = sp * kFewWaves + w;
   const int first = (int)((int64_t)gw * nu / nw), end = (int)((int64_t)(gw + 1) * nu / nw);
   const int* trow = a.g.table + (size_t)b * a.g.max_pages;
-  float* lg = a.logit ? a.logit + ((size_t)((size_t)b * a.g.Hkv + j) * kFewRows + hl) * a.logit_stride + 8 * G
+  float* lg = a.logit ? a.logit + ((size_t)((size_t)b * a.g.Hkv + j) * a.logit_rows + hl) * a.logit_stride + 8 * G
                       : nullptr;
   if (lg && hl >= rows) lg = nullptr;
   Unit<FMT> r0, r1;
@@ -444,7 +444,7 @@ __device__ __forceinline__ void store_k(const Stage<FMT, U>& g, ManyLds& m, int 
   if constexpr (FMT != kBf16) {   // finite and positive, so that hidden scores stay -inf
     const int there = g.page < 0 ? 0 : n_kv - (tile * kKeyTile + kg * U);
     if (chunk < U) {
-      m.ks[buf][kg * U + chunk] = (chunk < there ? fmaxf(g.ks, 1e-30f) : 1.0f) * c_log2;
+      m.ks[buf][kg * U + chunk] = chunk < there ? fmaxf(g.ks * c_log2, 1e-37f) : c_log2;
       m.vs[buf][kg * U + chunk] = chunk < there ? g.vs : 0.0f;
     }
   }
@@ -531,8 +531,8 @@ __device__ __forceinline__ v8bf read_v(const v4u* vt, int lane_part, int o, int 
 // The reference of a row's weights is the maximum of the first tile it sees;
 // later tiles need no maximum of their own: bf16 weights keep their precision
 // at any size, so the reference moves only when a lane's weights of a tile sum
-// to more than 2^60.
-constexpr float kFarSum = 0x1p60f;
+// to more than 2^16 (which leaves the accumulators their range).
+constexpr float kFarSum = 0x1p16f;
 
 template <int FMT, int NW>
 __global__ void __launch_bounds__(NW * 64, 2)
@@ -820,7 +820,7 @@ paged_few_finish_kernel(AttnArgs a) {
   }
   __syncthreads();
   if (key >= sq.n_kv) return;
-  const float* lg = a.logit + ((size_t)b * a.g.Hkv + j) * kFewRows * a.logit_stride + key;
+  const float* lg = a.logit + ((size_t)b * a.g.Hkv + j) * a.logit_rows * a.logit_stride + key;
   v4f sum = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll 4
   for (int r = 0; r < rows; ++r) {
@@ -872,10 +872,11 @@ paged_many_mass_kernel(AttnArgs a) {
       kf[c] = __builtin_bit_cast(v8bf, to_bf16<FMT>(*reinterpret_cast<const typename Eight<FMT>::type*>(
                                            src + (2 * c + hf) * (row_bytes<FMT>() / 16))));
     float ks = 1.0f;
-    if constexpr (FMT != kBf16) ks = fmaxf(a.ks[row], 1e-30f);   // hidden scores stay -inf
+    if constexpr (FMT != kBf16) ks = a.ks[row];
 #pragma unroll
     for (int e = 0; e < 16; ++e) {
-      kse[e] = FMT == kBf16 ? a.c_log2 : __shfl(ks, 8 * (e >> 2) + 4 * hf + (e & 3), 64) * a.c_log2;
+      // positive, so that hidden scores stay -inf
+      kse[e] = FMT == kBf16 ? a.c_log2 : fmaxf(__shfl(ks, 8 * (e >> 2) + 4 * hf + (e & 3), 64) * a.c_log2, 1e-37f);
       sum[e] = 0.0f;
     }
   }
@@ -960,7 +961,7 @@ struct Plan {
   int waves;           // of a workgroup of the many-row kernel (32 rows each)
   int row_tiles;       // row tiles of a sequence there
   int64_t n_kv;        // bound on a sequence's slots
-  int logit_stride;
+  int logit_rows, logit_stride;
   size_t part, logit, stat;   // workspace bytes
   size_t total() const { return part + logit + stat; }
 };
@@ -970,7 +971,7 @@ size_t up256(size_t x) { return (x + 255) & ~(size_t)255; }
 Plan plan_of(const hyq_pcache& c, const hyq_pbatch& b, int mass) {
   Plan p = {};
   const int g = c.Hq / c.Hkv;
-  const int rows = b.max_new * g;   // not of T: the workspace then grows with T
+  const int rows = std::max(b.max_new, 1) * g;   // not of T: the workspace then only grows with T
   p.many = rows > kFewRows;
   p.few = !p.many || b.B > 1;   // a mixed batch may hold single tokens
   p.few_max = p.few ? kFewRows : 0;
@@ -979,9 +980,15 @@ Plan plan_of(const hyq_pcache& c, const hyq_pbatch& b, int mass) {
   const int64_t units = std::max<int64_t>(1, (p.n_kv + kUnit - 1) / kUnit);
   const int64_t ktiles = std::max<int64_t>(1, (p.n_kv + kKeyTile - 1) / kKeyTile);
   p.S_few = (int)std::max<int64_t>(1, std::min({(512 + heads - 1) / heads, (units + 7) / 8, (int64_t)64}));
+  // Up to 128 rows, and below 4096 slots, workgroups of 128 rows (two to a CU)
+  // balance better: 2048 tokens from nothing 61 us against 66 with 256 rows, 8 x
+  // 200 over 1000 slots 44 and 47, 4 x 8 over 9001 33 and 40.  Longer scans gain
+  // more from eight waves sharing a tile's staging: 3 x 2k over 6011 int8 slots
+  // 839 and 966, 512 over 32k 276 and 295, 100 over 16k 50 and 52.
   p.waves = rows <= 128 || p.n_kv < 4096 ? 4 : 8;
-  p.row_tiles = (rows + p.waves * 32 - 1) / (p.waves * 32);
-  const int64_t wg = heads * p.row_tiles;
+  const int64_t wg = heads * ((rows + p.waves * 32 - 1) / (p.waves * 32));
+  const int launched = std::min(b.max_new, b.T) * g;   // the grid (the splits go by max_new alone)
+  p.row_tiles = (launched + p.waves * 32 - 1) / (p.waves * 32);
   p.S_many = (int)std::max<int64_t>(1, std::min({(p.waves == 4 ? 512 : 256) / wg, (ktiles + 7) / 8, (int64_t)64}));
   p.join_few = p.few && (p.S_few > 1 || mass);
   p.join_many = p.many && p.S_many > 1;
@@ -991,8 +998,9 @@ Plan plan_of(const hyq_pcache& c, const hyq_pbatch& b, int mass) {
   if (mass) {
     if (p.many) p.stat = up256(qrows * sizeof(float2));
     if (p.few) {
+      p.logit_rows = p.many ? kFewRows : rows;
       p.logit_stride = (int)(units * kUnit);
-      p.logit = up256((size_t)heads * kFewRows * p.logit_stride * 4);
+      p.logit = up256((size_t)heads * p.logit_rows * p.logit_stride * 4);
     }
   }
   return p;
@@ -1019,6 +1027,11 @@ hipError_t launch(const Plan& p, const AttnArgs& a, hipStream_t st) {
 }
 
 }  // namespace
+
+bool paged_grid_fits(const hyq_pcache& c, const hyq_pbatch& b) {
+  const Plan p = plan_of(c, b, HYQ_MASS_NONE);
+  return (int64_t)b.B * c.Hkv * p.row_tiles * p.S_many <= (int64_t)1 << 22;
+}
 
 size_t paged_ws_bytes(const hyq_pcache& c, const hyq_pbatch& b, int mass) {
   return plan_of(c, b, mass).total();
@@ -1048,6 +1061,7 @@ hipError_t launch_paged_attn(const hyq_pcache& c, const hyq_pbatch& b, const uin
   char* w = static_cast<char*>(ws);
   if (p.part) a.part = reinterpret_cast<float*>(w);
   if (p.logit) a.logit = reinterpret_cast<float*>(w + p.part);
+  a.logit_rows = p.logit_rows;
   a.logit_stride = p.logit_stride;
   if (p.stat) a.stat = reinterpret_cast<float2*>(w + p.part + p.logit);
   if (c.bits_kv == 16) return launch<kBf16>(p, a, st);

@@ -117,3 +117,45 @@ def test_missing_pages():
             np.testing.assert_array_equal(k[to[0], 0, to[1]], row)
     assert np.array_equal(k[6, 0, 8:], was[6, 0, 8:])
     assert np.array_equal(k[[1, 3, 4, 7]], was[[1, 3, 4, 7]])
+
+
+def test_shared_old_pages():
+    """Two sequences with the same prompt pages, evicted in one call: the old
+    pages are only read."""
+    import torch
+    rng = np.random.default_rng(2)
+    bufs, _ = pc.pool(rng, "int8", 12, 2, 16)
+    mass = rng.random((12, 2, 16)).astype(np.float32)
+    table = np.array([[0, 1, 2], [0, 1, 3]], dtype=np.int32)
+    new_table = np.array([[5, 6], [7, 8]], dtype=np.int32)
+    cache = pc.cache_of(bufs, "int8", 2, mass)
+    keep = torch.empty((2, 2, 20), dtype=torch.int32, device="cuda")
+    new_lens = torch.empty((2,), dtype=torch.int32, device="cuda")
+    hyq.hyq_evict(cache, pc.dev(np.array([48, 40], np.int32)), pc.dev(table), pc.dev(new_table), keep,
+                  new_lens, max_len=48, budget=20, recent=3)
+    want, _ = po.evict(mass, [48, 40], table, 20, 3)
+    np.testing.assert_array_equal(keep.cpu().numpy(), want)
+    k = cache.bufs["k"].cpu().numpy()
+    for b in range(2):
+        for j in range(2):
+            for i, s in enumerate(want[b, j]):
+                assert np.array_equal(k[new_table[b, i // 16], j, i % 16], bufs["k"][table[b, s // 16], j, s % 16])
+    assert np.array_equal(k[:5], bufs["k"][:5]) and np.array_equal(k[9:], bufs["k"][9:])
+
+
+def test_lengths_beyond_their_bound():
+    """Device lengths outside [0, max_len] count as the nearest bound."""
+    import torch
+    rng = np.random.default_rng(3)
+    bufs, _ = pc.pool(rng, "bf16", 16, 1, 16)
+    mass = rng.random((16, 1, 16)).astype(np.float32)
+    table = np.arange(8, dtype=np.int32).reshape(2, 4)
+    new_table = np.array([[9], [10]], dtype=np.int32)
+    cache = pc.cache_of(bufs, "bf16", 1, mass)
+    keep = torch.empty((2, 1, 10), dtype=torch.int32, device="cuda")
+    new_lens = torch.empty((2,), dtype=torch.int32, device="cuda")
+    hyq.hyq_evict(cache, pc.dev(np.array([-5, 1 << 30], np.int32)), pc.dev(table), pc.dev(new_table), keep,
+                  new_lens, max_len=50, budget=10, recent=2)
+    want, lens = po.evict(mass, [0, 50], table, 10, 2)
+    np.testing.assert_array_equal(keep.cpu().numpy(), want)
+    np.testing.assert_array_equal(new_lens.cpu().numpy(), lens)

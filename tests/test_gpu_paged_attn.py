@@ -106,10 +106,10 @@ def test_looser_bounds_change_nothing(case):
 
 
 @pytest.mark.parametrize("fmt", ["bf16", "fp8", "int8"])
-@pytest.mark.parametrize("new", [1, 40])
-def test_holes_and_poison(fmt, new):
+@pytest.mark.parametrize("new,max_len", [(1, 100), (40, 100), (40, 9000)])
+def test_holes_and_poison(fmt, new, max_len):
     """Keys of missing pages take no part; what lies behind the sequences and in
-    pages of nobody may be NaN."""
+    pages of nobody may be NaN.  (A bound of 9000 slots: workgroups of 8 waves.)"""
     import torch
     for hole in ((0, 0, -1), (0, 2, 1 << 29), (0, 6, -7)):
         case = ([100], [new], 4, 1, 16, fmt, 0, "set")
@@ -127,7 +127,7 @@ def test_holes_and_poison(fmt, new):
                     r["bufs"][name].transpose(0, 2, 1, 3)[~owned] = 0x7F   # NaN
                 r["bufs"][name + "_scale"].transpose(0, 2, 1)[~owned] = np.nan
         cache = pc.cache_of(r["bufs"], fmt, 4, r["mass"])
-        batch = pc.batch_of(r["cu"], r["lens"], r["table"])
+        batch = pc.batch_of(r["cu"], r["lens"], r["table"], max_len=max_len)
         out = torch.empty((new, 4, D), dtype=torch.float32, device="cuda")
         hyq.hyq_paged_attn(cache, batch, pc.dev(r["q"]), out, mass=hyq.MASS_SET,
                            ws=pc.workspace(cache, batch, True, new))
@@ -151,8 +151,8 @@ def test_rows_that_see_nothing(new):
     assert np.array_equal(cache.bufs["mass"].cpu().numpy(), r["mass"])
 
 
-@pytest.mark.parametrize("new", [2, 60])
-def test_extreme_logits(new):
+@pytest.mark.parametrize("new,max_len", [(2, 90), (60, 90), (80, 9000)])
+def test_extreme_logits(new, max_len):
     """Logits of a few thousand either way: one key takes all the weight, and
     rows whose logits are all far below zero are still a softmax."""
     import torch
@@ -165,11 +165,151 @@ def test_extreme_logits(new):
     cu = np.array([0, new])
     want = po.attention(po.bf16(q), vals["k"], vals["v"], cu, lens, table, 1, SCALE)
     cache = pc.cache_of(bufs, "bf16", 2)
-    batch = pc.batch_of(cu, lens, table)
+    batch = pc.batch_of(cu, lens, table, max_len=max_len)
     out = torch.empty((new, 2, D), device="cuda")
     hyq.hyq_paged_attn(cache, batch, pc.dev(q), out, ws=pc.workspace(cache, batch, False, new))
     atol, rtol = pc.out_tolerance(po.bf16(q), vals, SCALE, 2 * new, False)
     np.testing.assert_allclose(pc.host(out), want, rtol=rtol, atol=atol)
+
+
+@pytest.mark.parametrize("new,max_len", [(1, 400), (30, 400), (70, 9000)])
+def test_rising_and_falling_logits(new, max_len):
+    """Keys along the query, each hundred far larger (or smaller) than the one
+    before: the reference of a row's weights has to follow."""
+    import torch
+    rng = np.random.default_rng(2)
+    g, page, n = 4, 32, 400
+    table, n_pages = pc.tables(rng, [n + new], page)
+    for sign in (1, -1):
+        bufs, _ = pc.pool(rng, "bf16", n_pages, 1, page)
+        q = np.zeros((new, g, D), dtype=np.float32)
+        q[..., 0] = 1 + rng.random((new, g))
+        k = po.bf16(bufs["k"])
+        for s in range(n + new):
+            p, o = po.place(table, 0, s, page, n_pages)
+            k[p, 0, o, 0] = sign * 700.0 * (s // 100) + 8 * rng.standard_normal()
+        bufs["k"] = hyq_bits(k)
+        qb = hyq_bits(q)
+        vals = dict(k=po.bf16(bufs["k"]), v=po.bf16(bufs["v"]))
+        mass = np.zeros((n_pages, 1, page), np.float32)
+        wm = mass.astype(np.float64)
+        cu = np.array([0, new])
+        want = po.attention(po.bf16(qb), vals["k"], vals["v"], cu, [n], table, 1, 1.0, wm, "set")
+        cache = pc.cache_of(bufs, "bf16", g, mass)
+        batch = pc.batch_of(cu, [n], table, max_len=max_len)
+        out = torch.empty((new, g, D), device="cuda")
+        hyq.hyq_paged_attn(cache, batch, pc.dev(qb), out, softmax_scale=1.0, mass=hyq.MASS_SET,
+                           ws=pc.workspace(cache, batch, True, new))
+        # one product (channel 0) carries the logits: exact to float32, up to 6000 (2^-11 absolute)
+        w = 2.0 ** -16 if new * g <= 16 else 2.0 ** -8
+        atol = (2.0 ** -9 + w) * np.abs(vals["v"]).max()
+        np.testing.assert_allclose(pc.host(out), want, rtol=2.0 ** -20, atol=atol)
+        got = pc.host(cache.bufs["mass"])
+        np.testing.assert_allclose(got[wm > 1e-30], wm[wm > 1e-30], rtol=2.0 ** -8)
+        assert np.all(got[wm < 1e-60] < 1e-30)
+
+
+def hyq_bits(x):
+    from paper_2608_27875_amd import gen
+    return gen.f32_to_bf16_bits(np.asarray(x, dtype=np.float32))
+
+
+def test_mixed_batch_with_splits():
+    """A long chunk and single tokens whose keys are split too: both kernels
+    leave partials in one workspace; masses of both."""
+    import torch
+    g = torch.Generator(device="cuda").manual_seed(3)
+    Hq, Hkv, page = 8, 2, 32
+    lens, news = [5000, 3001, 0, 4100], [33, 1, 20, 2]
+    cu = [0, 33, 34, 54, 56]
+    used = [-(-(a + n) // page) for a, n in zip(lens, news)]
+    perm = torch.randperm(sum(used) + 1, generator=g, device="cuda").to(torch.int32)
+    k = torch.randn((sum(used) + 1, Hkv, page, D), generator=g, device="cuda").bfloat16()
+    v = torch.randn((sum(used) + 1, Hkv, page, D), generator=g, device="cuda").bfloat16()
+    q = torch.randn((56, Hq, D), generator=g, device="cuda").bfloat16()
+    mass = torch.zeros((sum(used) + 1, Hkv, page), device="cuda")
+    table = torch.full((4, max(used)), -1, dtype=torch.int32, device="cuda")
+    for b, u in enumerate(used):
+        table[b, :u] = perm[sum(used[:b]):sum(used[:b + 1])]
+    cache = hyq.PagedCache(Hq=Hq, Hkv=Hkv, page=page, n_pages=k.shape[0], device=k.device,
+                           bufs=dict(k=k, v=v, mass=mass))
+    batch = pc.batch_of(cu, lens, table.cpu().numpy())
+    out = torch.empty((56, Hq, D), device="cuda")
+    hyq.hyq_paged_attn(cache, batch, q, out, mass=hyq.MASS_SET, ws=pc.workspace(cache, batch, True, 56))
+    e = 130 * 2.0 ** -24 * SCALE * 128 * 30   # as in test_long
+    for b in range(4):
+        p = table[b, :used[b]].long()
+        n = lens[b] + news[b]
+        kk, vv = (x[p].transpose(0, 1).reshape(Hkv, -1, D)[:, :n] for x in (k, v))
+        want, wm = plain(q[cu[b]:cu[b + 1]], kk, vv, lens[b])
+        w = 2.0 ** -16 if news[b] * 4 <= 16 else 2.0 ** -8
+        off = (out[cu[b]:cu[b + 1]].double() - want).abs().max()
+        assert float(off) <= (2 * e + w) * float(v.float().abs().max())
+        got = mass[p].transpose(0, 1).reshape(Hkv, -1)[:, :n]
+        np.testing.assert_allclose(pc.host(got), wm.cpu().numpy(), rtol=2 * e + 2.0 ** -18)
+
+
+@pytest.mark.parametrize("fmt", ["int8", "fp8"])
+def test_long_codes(fmt):
+    """8-bit pages in a long chunk (eight waves, splits): against float64 on
+    what the codes stand for."""
+    import torch
+    g = torch.Generator(device="cuda").manual_seed(9)
+    Hq, Hkv, page, len0, new = 5, 1, 64, 6500, 301
+    pages = -(-(len0 + new) // page)
+    rows = (pages, Hkv, page)
+    if fmt == "int8":
+        codes = [torch.randint(-127, 128, rows + (D,), generator=g, device="cuda").to(torch.int8) for _ in "kv"]
+        vals = [c.double() for c in codes]
+    else:
+        codes = [(torch.randn(rows + (D,), generator=g, device="cuda") * 150).clamp(-448, 448)
+                 .to(torch.float8_e4m3fn) for _ in "kv"]
+        vals = [c.float().double() for c in codes]
+    scales = [torch.rand(rows, generator=g, device="cuda") / 60 for _ in "kv"]
+    scales[0][0, 0, 3] = 0   # a row of zeros
+    codes = [c.view(torch.uint8) for c in codes]
+    codes[0][0, 0, 3] = 0
+    vals[0][0, 0, 3] = 0
+    k, v = (x * s[..., None].double() for x, s in zip(vals, scales))
+    bits, kind = pc.FORMATS[fmt]
+    mass = torch.zeros(rows, device="cuda")
+    cache = hyq.PagedCache(Hq=Hq, Hkv=Hkv, page=page, n_pages=pages, device=mass.device, bits_kv=bits,
+                           kv_format=kind, bufs=dict(k=codes[0], v=codes[1], k_scale=scales[0],
+                                                     v_scale=scales[1], mass=mass))
+    q = torch.randn((new, Hq, D), generator=g, device="cuda").bfloat16()
+    batch = pc.batch_of([0, new], [len0], np.arange(pages, dtype=np.int32)[None])
+    out = torch.empty((new, Hq, D), device="cuda")
+    hyq.hyq_paged_attn(cache, batch, q, out, mass=hyq.MASS_SET, ws=pc.workspace(cache, batch, True, new))
+    kk, vv = (x.transpose(0, 1).reshape(Hkv, -1, D)[:, :len0 + new] for x in (k, v))
+    want, wm = plain(q, kk, vv, len0)
+    big = float(q.double().abs().amax((0, 1)) @ kk[0].abs().amax(0))
+    e = SCALE * big * 130 * 2.0 ** -24
+    # the worst case of 2^-8 a weight, and a mean error far below it
+    assert float((out.double() - want).abs().max()) <= (2 * e + 2.0 ** -8) * float(vv.abs().max())
+    assert float((out.double() - want).norm()) <= 2.0 ** -8 * float(want.norm()) + 2 * e * float(vv.abs().max())
+    got = mass.transpose(0, 1).reshape(Hkv, -1)[:, :len0 + new]
+    np.testing.assert_allclose(pc.host(got), wm.cpu().numpy(), rtol=2 * e + 2.0 ** -18)
+
+
+def test_two_streams_at_once():
+    """Two steps in flight on two streams, each with its own workspace."""
+    import torch
+    r = [reference(c, seed=4) for c in (CASES[10], CASES[3])]
+    cases = [CASES[10], CASES[3]]
+    jobs = []
+    for c, x in zip(cases, r):
+        cache = pc.cache_of(x["bufs"], c[5], c[2], x["mass"])
+        batch = pc.batch_of(x["cu"], x["lens"], x["table"], max_len=6000)
+        out = torch.empty((x["T"], c[2], D), device="cuda")
+        jobs.append((cache, batch, pc.dev(x["q"]), out, pc.workspace(cache, batch, True, x["T"]),
+                     torch.cuda.Stream()))
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for cache, batch, q, out, ws, st in jobs:
+            hyq.hyq_paged_attn(cache, batch, q, out, mass=hyq.MASS_SET, ws=ws, stream=st)
+    torch.cuda.synchronize()
+    for c, x, (cache, _, _, out, _, _) in zip(cases, r, jobs):
+        check(c[:6] + (0, "set"), x, cache, out)
 
 
 def plain(q, k, v, len0):

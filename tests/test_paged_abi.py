@@ -52,7 +52,7 @@ BAD_BUFFERS = [(dict(k=None), EINVAL), (dict(v=None), EINVAL), (dict(k=FAKE + 8)
 BAD_BATCH = [
     (dict(B=0), EINVAL), (dict(T=-1), EINVAL), (dict(max_new=-1), EINVAL), (dict(max_len=-1), EINVAL),
     (dict(max_pages=0), EINVAL), (dict(max_len=1 << 23), EUNSUP), (dict(T=1 << 24), EUNSUP),
-    (dict(B=20000), EUNSUP), (dict(cu_new=None), EINVAL), (dict(lens=None), EINVAL),
+    (dict(B=20000), EUNSUP), (dict(B=16000, T=1 << 20, max_new=1 << 20), EUNSUP), (dict(cu_new=None), EINVAL), (dict(lens=None), EINVAL),
     (dict(table=None), EINVAL),
 ]
 BAD_ROPE = [
@@ -152,7 +152,7 @@ def test_bad_evictions(lib, kw):
 
 
 def test_too_large_evictions(lib):
-    assert evict(lib, max_len=(1 << 23) + 1) == EUNSUP
+    assert evict(lib, max_len=(1 << 22) + 1) == EUNSUP
     assert evict(lib, B=20000) == EUNSUP
 
 
