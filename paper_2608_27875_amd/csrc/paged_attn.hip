@@ -36,8 +36,8 @@ typedef unsigned v2u __attribute__((ext_vector_type(2)));
 constexpr int kBf16 = -1;            // page format beside HYQ_FMT_INT / HYQ_FMT_FP8 (8-bit codes)
 constexpr int kFewRows = 16;         // rows per KV head of the few-row kernel
 constexpr int kFewThreads = 256, kFewWaves = 4, kUnit = 32;
+constexpr int kFewSplits = 256;      // most splits of a sequence's keys there
 constexpr int kKeyTile = 64;         // keys of a tile of the many-row kernel
-constexpr int kPart = kHeadDim + 4;  // floats of a partial: acc[128], max, sum, padding
 constexpr float kLazy = 8.0f;        // rescale only when the maximum grows by more than 2^8
 constexpr float kNever = 3.0e38f;    // the "maximum" of a row that sees nothing: exp2(z - it) is 0
 constexpr float kFloor = -1.0e30f;   // start of a running maximum (finite: exp2 of -inf - it is 0)
@@ -55,7 +55,9 @@ struct AttnArgs {
   int few_max;         // sequences of at most so many rows go to the few-row kernel
   int S_few, S_many;   // splits of the keys in the two kernels
   int join_few;        // whether the few-row kernel leaves partials
-  float* part;         // [S][T][Hq][kPart]
+  float* part;         // partial sums over a split's keys [S][T][Hq][kHeadDim]
+  float2* part_ml;     // their (max, sum) [T][Hq][S]
+  int S_part;          // S of the two: the larger of the splits
   float* logit;        // few rows with mass: [B][Hkv][logit_rows][logit_stride]
   int logit_rows, logit_stride;
   uint32_t inv_g;      // ceil(2^32 / g) (g > 1): r / g for the rows of a step
@@ -386,9 +388,8 @@ paged_few_kernel(AttnArgs a) {
     const int ii = rw / a.g.g;
     const size_t row = (size_t)(sq.t0 + ii) * a.g.Hq + (size_t)j * a.g.g + (rw - ii * a.g.g);
     if (a.join_few) {
-      float* dst = a.part + ((size_t)sp * a.g.T * a.g.Hq + row) * kPart;
-      *reinterpret_cast<v4f*>(dst + ch) = acc;
-      if (ch == 0) *reinterpret_cast<float2*>(dst + kHeadDim) = make_float2(M, sum);
+      *reinterpret_cast<v4f*>(a.part + ((size_t)sp * a.g.T * a.g.Hq + row) * kHeadDim + ch) = acc;
+      if (ch == 0) a.part_ml[row * a.S_part + sp] = make_float2(M, sum);
     } else {
       store4(a, row, ch, acc * (sum > 0.0f ? 1.0f / sum : 0.0f));
     }
@@ -707,14 +708,14 @@ paged_many_kernel(AttnArgs a, const int32_t* __restrict__ table, int tiles) {
   l += __shfl_xor(l, 32, 64);
   if (r_mine >= rows) return;
   if (a.S_many > 1) {
-    float* dst = a.part + ((size_t)sp * a.g.T * a.g.Hq + qrow) * kPart;
+    float* dst = a.part + ((size_t)sp * a.g.T * a.g.Hq + qrow) * kHeadDim;
 #pragma unroll
     for (int d = 0; d < 4; ++d)
 #pragma unroll
       for (int e = 0; e < 4; ++e)
         *reinterpret_cast<v4f*>(dst + d * 32 + e * 8 + hf * 4) =
             v4f{acc[d][4 * e], acc[d][4 * e + 1], acc[d][4 * e + 2], acc[d][4 * e + 3]};
-    if (hf == 0) *reinterpret_cast<float2*>(dst + kHeadDim) = make_float2(m, l);
+    if (hf == 0) a.part_ml[(size_t)qrow * a.S_part + sp] = make_float2(m, l);
   } else {
     const float inv = l > 0.0f ? 1.0f / l : 0.0f;
 #pragma unroll
@@ -731,23 +732,28 @@ paged_many_kernel(AttnArgs a, const int32_t* __restrict__ table, int tiles) {
 // Joining the splits, and masses.
 // ---------------------------------------------------------------------------
 
-constexpr int kJoinThreads = 128, kJoinShares = kJoinThreads / 32;
-constexpr int kMassKeys = kJoinThreads * 4;   // keys of a mass workgroup of the few-row path
+constexpr int kJoinThreads = 128;     // chunks: at most 64 splits, in practice a handful
+constexpr int kFinishThreads = 256;   // few rows: up to kFewSplits
+constexpr int kStatThreads = kFinishThreads / kFewRows;   // threads that join a row's maximum and sum
+constexpr int kMassKeys = kFinishThreads * 4;   // keys of a mass workgroup of the few-row path
 
-// Row `row` (token * Hq + head) of the output from its S partials: 4 shares of
+// Row `row` (token * Hq + head) of the output from its S partials: shares of
 // them, 32 lanes of 4 channels each, joined through LDS.
+template <int THREADS>
 __device__ __forceinline__ void join_row(const AttnArgs& a, size_t row, int S) {
-  __shared__ v4f x_acc[kJoinShares][32];
-  __shared__ float x_m[kJoinShares], x_l[kJoinShares];
+  constexpr int kShares = THREADS / 32;
+  __shared__ v4f x_acc[kShares][32];
+  __shared__ float x_m[kShares], x_l[kShares];
   const int c4 = threadIdx.x & 31, ph = threadIdx.x >> 5;
-  const float* base = a.part + row * kPart;
-  const size_t stride = (size_t)a.g.T * a.g.Hq * kPart;
+  const float* base = a.part + row * kHeadDim + c4 * 4;
+  const size_t stride = (size_t)a.g.T * a.g.Hq * kHeadDim;
+  const float2* mls = a.part_ml + row * a.S_part;
   float M = kFloor, L = 0.0f;
   v4f acc = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll 4
-  for (int s = ph; s < S; s += kJoinShares) {
-    const v4f x = *reinterpret_cast<const v4f*>(base + s * stride + c4 * 4);
-    const float2 ml = *reinterpret_cast<const float2*>(base + s * stride + kHeadDim);
+  for (int s = ph; s < S; s += kShares) {
+    const v4f x = *reinterpret_cast<const v4f*>(base + s * stride);
+    const float2 ml = mls[s];
     const float mn = fmaxf(M, ml.x);
     const float f = __builtin_amdgcn_exp2f(M - mn), e = __builtin_amdgcn_exp2f(ml.x - mn);
     acc = acc * f + x * e;
@@ -762,7 +768,7 @@ __device__ __forceinline__ void join_row(const AttnArgs& a, size_t row, int S) {
   __syncthreads();
   if (ph != 0) return;
 #pragma unroll
-  for (int s = 1; s < kJoinShares; ++s) {
+  for (int s = 1; s < kShares; ++s) {
     const float mn = fmaxf(M, x_m[s]);
     const float f = __builtin_amdgcn_exp2f(M - mn), e = __builtin_amdgcn_exp2f(x_m[s] - mn);
     acc = acc * f + x_acc[s][c4] * e;
@@ -782,15 +788,17 @@ paged_join_kernel(AttnArgs a) {
   if (b < 0) return;
   const Seq sq = seq_of(a.g, b);
   if (t - sq.t0 >= sq.n_new || sq.n_new * a.g.g <= a.few_max) return;
-  join_row(a, blockIdx.x, a.S_many);
+  join_row<kJoinThreads>(a, blockIdx.x, a.S_many);
 }
 
-// After the few-row kernel (one launch for both, 14.9 us at 16 x 32k slots; 33 as
-// two): workgroups (b, j, y) with y < kFewRows join query
-// row y; the others (with masses) take 512 keys each: the maximum and the sum
-// of every row from the partials, then the weights from the stored logits (4
-// keys a thread, rows in order).
-__global__ void __launch_bounds__(kJoinThreads)
+// After the few-row kernel (one launch for both, 16 us at 16 x 32k slots; 33 as
+// two): workgroups (b, j, y) with y < kFewRows join query row y; the others
+// (with masses) take 1024 keys each: the maximum and the sum of every row from
+// the partials, then the weights from the stored logits (4 keys a thread, rows in
+// order).  Maxima and sums of a row lie together (32768 slots, 32 heads over 8:
+// 26.8 us, 27.6 inside the partials); 16 threads join them for the masses (65536
+// E4M3 slots, 8 heads over 2, 128 splits: 27 us with 4 threads, 19 with 8).
+__global__ void __launch_bounds__(kFinishThreads)
 paged_few_finish_kernel(AttnArgs a) {
   const int j = blockIdx.x % a.g.Hkv, b = blockIdx.x / a.g.Hkv;
   const Seq sq = seq_of(a.g, b);
@@ -801,31 +809,31 @@ paged_few_finish_kernel(AttnArgs a) {
     return (size_t)(sq.t0 + i) * a.g.Hq + (size_t)j * a.g.g + (r - i * a.g.g);
   };
   if (blockIdx.y < kFewRows) {
-    if ((int)blockIdx.y < rows) join_row(a, row_of(blockIdx.y), a.S_few);
+    if ((int)blockIdx.y < rows) join_row<kFinishThreads>(a, row_of(blockIdx.y), a.S_few);
     return;
   }
   const int key = (blockIdx.y - kFewRows) * kMassKeys + (int)threadIdx.x * 4;
   if (key - (int)threadIdx.x * 4 >= sq.n_kv) return;
   __shared__ float2 st[kFewRows];
-  if ((int)threadIdx.x < rows * 4) {   // 4 threads a row (at most 64: one wave)
-    const int r = threadIdx.x >> 2;
-    const float* base = a.part + row_of(r) * kPart + kHeadDim;
-    const size_t stride = (size_t)a.g.T * a.g.Hq * kPart;
+  if ((int)threadIdx.x < rows * kStatThreads) {
+    const int r = threadIdx.x / kStatThreads;
+    const float2* mls = a.part_ml + row_of(r) * a.S_part;
     float M = kFloor, L = 0.0f;
-    for (int s = threadIdx.x & 3; s < a.S_few; s += 4) {
-      const float2 ml = *reinterpret_cast<const float2*>(base + s * stride);
+#pragma unroll 8
+    for (int s = threadIdx.x % kStatThreads; s < a.S_few; s += kStatThreads) {
+      const float2 ml = mls[s];
       const float mn = fmaxf(M, ml.x);
       L = L * __builtin_amdgcn_exp2f(M - mn) + ml.y * __builtin_amdgcn_exp2f(ml.x - mn);
       M = mn;
     }
 #pragma unroll
-    for (int o = 1; o < 4; o <<= 1) {
+    for (int o = 1; o < kStatThreads; o <<= 1) {
       const float m2 = __shfl_xor(M, o, 64), l2 = __shfl_xor(L, o, 64);
       const float mn = fmaxf(M, m2);
       L = L * __builtin_amdgcn_exp2f(M - mn) + l2 * __builtin_amdgcn_exp2f(m2 - mn);
       M = mn;
     }
-    if ((threadIdx.x & 3) == 0) st[r] = make_float2(L > 0.0f ? M : kNever, L > 0.0f ? 1.0f / L : 0.0f);
+    if (threadIdx.x % kStatThreads == 0) st[r] = make_float2(L > 0.0f ? M : kNever, L > 0.0f ? 1.0f / L : 0.0f);
   }
   __syncthreads();
   if (key >= sq.n_kv) return;
@@ -972,8 +980,9 @@ struct Plan {
   int row_tiles;       // row tiles of a sequence there
   int64_t n_kv;        // bound on a sequence's slots
   int logit_rows, logit_stride;
-  size_t part, logit, stat;   // workspace bytes
-  size_t total() const { return part + logit + stat; }
+  int S_part;          // splits whose partials are kept
+  size_t part, ml, logit, stat;   // workspace bytes
+  size_t total() const { return part + ml + logit + stat; }
 };
 
 size_t up256(size_t x) { return (x + 255) & ~(size_t)255; }
@@ -989,7 +998,11 @@ Plan plan_of(const hyq_pcache& c, const hyq_pbatch& b, int mass) {
   const int64_t heads = (int64_t)b.B * c.Hkv;
   const int64_t units = std::max<int64_t>(1, (p.n_kv + kUnit - 1) / kUnit);
   const int64_t ktiles = std::max<int64_t>(1, (p.n_kv + kKeyTile - 1) / kKeyTile);
-  p.S_few = (int)std::max<int64_t>(1, std::min({(512 + heads - 1) / heads, (units + 7) / 8, (int64_t)64}));
+  // Two workgroups to a CU, at least 8 units each; one KV head fills the chip by
+  // itself from 2048 units on (131072 slots, 8 heads over 1: 19.9 us with 256
+  // splits at most, 25.7 with 128, 41 with 64; 65536 E4M3 slots, 8 over 2, with
+  // masses: 20.0, 18.3 and 28).
+  p.S_few = (int)std::max<int64_t>(1, std::min({(512 + heads - 1) / heads, (units + 7) / 8, (int64_t)kFewSplits}));
   // Up to 128 rows, and below 4096 slots, workgroups of 128 rows (two to a CU)
   // balance better: 2048 tokens from nothing 61 us against 66 with 256 rows, 8 x
   // 200 over 1000 slots 44 and 47, 4 x 8 over 9001 33 and 40.  Longer scans gain
@@ -1002,9 +1015,10 @@ Plan plan_of(const hyq_pcache& c, const hyq_pbatch& b, int mass) {
   p.S_many = (int)std::max<int64_t>(1, std::min({(p.waves == 4 ? 512 : 256) / wg, (ktiles + 7) / 8, (int64_t)64}));
   p.join_few = p.few && (p.S_few > 1 || mass);
   p.join_many = p.many && p.S_many > 1;
-  const int S = std::max(p.join_few ? p.S_few : 0, p.join_many ? p.S_many : 0);
+  p.S_part = std::max(p.join_few ? p.S_few : 0, p.join_many ? p.S_many : 0);
   const size_t qrows = (size_t)b.T * c.Hq;
-  p.part = up256((size_t)S * qrows * kPart * 4);
+  p.part = up256((size_t)p.S_part * qrows * kHeadDim * 4);
+  p.ml = up256((size_t)p.S_part * qrows * sizeof(float2));
   if (mass) {
     if (p.many) p.stat = up256(qrows * sizeof(float2));
     if (p.few) {
@@ -1028,7 +1042,7 @@ hipError_t launch(const Plan& p, const AttnArgs& a, hipStream_t st) {
   const bool mass = a.mass_mode != HYQ_MASS_NONE;
   if (p.join_few) {
     const unsigned keys = mass ? (unsigned)((p.n_kv + kMassKeys - 1) / kMassKeys) : 0u;
-    paged_few_finish_kernel<<<dim3(heads, kFewRows + keys), kJoinThreads, 0, st>>>(a);
+    paged_few_finish_kernel<<<dim3(heads, kFewRows + keys), kFinishThreads, 0, st>>>(a);
   }
   if (p.join_many) paged_join_kernel<<<(unsigned)(a.g.T * a.g.Hq), kJoinThreads, 0, st>>>(a);
   if (p.many && mass)
@@ -1070,10 +1084,15 @@ hipError_t launch_paged_attn(const hyq_pcache& c, const hyq_pbatch& b, const uin
   a.join_few = p.join_few;
   char* w = static_cast<char*>(ws);
   if (p.part) a.part = reinterpret_cast<float*>(w);
-  if (p.logit) a.logit = reinterpret_cast<float*>(w + p.part);
+  w += p.part;
+  if (p.ml) a.part_ml = reinterpret_cast<float2*>(w);
+  w += p.ml;
+  a.S_part = p.S_part;
+  if (p.logit) a.logit = reinterpret_cast<float*>(w);
+  w += p.logit;
   a.logit_rows = p.logit_rows;
   a.logit_stride = p.logit_stride;
-  if (p.stat) a.stat = reinterpret_cast<float2*>(w + p.part + p.logit);
+  if (p.stat) a.stat = reinterpret_cast<float2*>(w);
   if (c.bits_kv == 16) return launch<kBf16>(p, a, st);
   if (c.kv_format == HYQ_FMT_FP8) return launch<HYQ_FMT_FP8>(p, a, st);
   return launch<HYQ_FMT_INT>(p, a, st);

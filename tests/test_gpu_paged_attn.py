@@ -331,7 +331,8 @@ def plain(q, k, v, len0):
 
 @pytest.mark.parametrize("len0,new,Hq,Hkv,page,fmt", [
     (32749, 1, 8, 2, 64, "bf16"), (20011, 3, 10, 2, 16, "bf16"), (9000, 777, 8, 2, 128, "bf16"),
-    (40001, 130, 5, 1, 256, "bf16"), (0, 1500, 4, 1, 32, "bf16"),
+    (40001, 130, 5, 1, 256, "bf16"), (0, 1500, 4, 1, 32, "bf16"), (131071, 1, 8, 1, 64, "bf16"),
+    (70003, 2, 4, 1, 16, "bf16"),
 ])
 def test_long(len0, new, Hq, Hkv, page, fmt):
     """Long sequences (many splits, many tiles), every output and mass."""
