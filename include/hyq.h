@@ -483,7 +483,8 @@ HYQ_API int hyq_pcache_init(int32_t Hq, int32_t Hkv, int32_t D, int32_t page, in
  * bf16, k and v rows into their slots (codes are taken of the float32 values,
  * not of bf16 ones); mass, where there is one, is 0 in those slots.
  * q, k, v: bf16 rows [T][heads][D] with strides as for hyq_norm_rope; pos
- * int32 [T].  q and q_out may be NULL together (keys and values only).
+ * int32 [T].  q_out must not overlap the inputs; q and q_out may be NULL together
+ * (keys and values only).
  * lens is not changed: hyq_paged_attn of the same step takes the same batch.
  */
 HYQ_API int hyq_paged_append(const hyq_pcache* cache, const hyq_pbatch* batch,
@@ -509,7 +510,8 @@ HYQ_API int hyq_paged_ws_bytes(const hyq_pcache* cache, const hyq_pbatch* batch,
  * With mass, for every slot n < lens[b] + new of a sequence with new tokens:
  *   mass[b][j][n] (+)= sum over its new tokens i and the g heads of group j of
  *                      the weight w_n / sum w that they give n.
- * q: bf16 [T][Hq][D]; out: [T][Hq][D], float32 (out_dtype 0) or bf16 (1).
+ * q: bf16 [T][Hq][D]; out: [T][Hq][D], float32 (out_dtype 0) or bf16 (1); out,
+ * q and ws must not overlap.
  * Precision: bf16 products (8-bit codes are exact in bf16, their scales are
  * applied in float32), float32 sums; the weights enter the products with V as
  * a high + low bf16 pair where a sequence has at most 16 query rows per KV

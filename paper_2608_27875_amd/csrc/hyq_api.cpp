@@ -274,6 +274,11 @@ int check_rows(const char* name, const void* p, int64_t stride, int heads, int D
   return HYQ_OK;
 }
 
+// Whether n bytes at out overlap rows of a norm_rope / append call.
+bool overlaps_rows(const void* out, size_t n, const void* p, int64_t stride, int heads, int D, int64_t T) {
+  return out && p && overlaps(out, n, p, ((size_t)(T - 1) * stride + (size_t)heads * D) * 2);
+}
+
 // Geometry of a paged cache, without its buffers.
 int check_pcache_geometry(const hyq_pcache* c) {
   if (!c) return fail(HYQ_EINVAL, "cache is NULL");
@@ -649,6 +654,19 @@ HYQ_API int hyq_norm_rope(const hyq_shape* shape, const hyq_rope* rope, const vo
   if ((int64_t)shape->B * shape->L * (shape->Hq + 2 * shape->Hkv) > kMaxRows)
     return fail(HYQ_EUNSUPPORTED, "%lld token rows in one call not supported",
                 (long long)shape->B * shape->L);
+  const int64_t T = (int64_t)shape->B * shape->L;
+  const struct {
+    const char* name;
+    const void* p;
+    int heads;
+  } outs[] = {{"Q", Q, shape->Hq}, {"K", K, shape->Hkv}, {"V", V, shape->Hkv}};
+  for (const auto& o : outs) {
+    const size_t n = (size_t)T * o.heads * shape->D * 2;
+    if (overlaps_rows(o.p, n, q, q_stride, shape->Hq, shape->D, T) ||
+        overlaps_rows(o.p, n, k, k_stride, shape->Hkv, shape->D, T) ||
+        overlaps_rows(o.p, n, v, v_stride, shape->Hkv, shape->D, T))
+      return fail(HYQ_EINVAL, "%s must not overlap the inputs (rows go to other places)", o.name);
+  }
   const hyq::RopeRows x = {static_cast<const uint16_t*>(q), static_cast<const uint16_t*>(k),
                            static_cast<const uint16_t*>(v), q_stride, k_stride, v_stride, pos};
   return hip_status(hyq::launch_norm_rope(*shape, *rope, x, static_cast<uint16_t*>(Q),
@@ -698,6 +716,11 @@ HYQ_API int hyq_paged_append(const hyq_pcache* cache, const hyq_pbatch* batch,
       (rc = check_rows("v", v, v_stride, cache->Hkv, cache->D)))
     return rc;
   if (!aligned16(q_out)) return fail(HYQ_EINVAL, "q_out must be aligned to 16 bytes");
+  const size_t q_bytes = (size_t)batch->T * cache->Hq * cache->D * 2;
+  if (overlaps_rows(q_out, q_bytes, q, q_stride, cache->Hq, cache->D, batch->T) ||
+      overlaps_rows(q_out, q_bytes, k, k_stride, cache->Hkv, cache->D, batch->T) ||
+      overlaps_rows(q_out, q_bytes, v, v_stride, cache->Hkv, cache->D, batch->T))
+    return fail(HYQ_EINVAL, "q_out must not overlap the inputs");
   const hyq::RopeRows x = {static_cast<const uint16_t*>(q), static_cast<const uint16_t*>(k),
                            static_cast<const uint16_t*>(v), q_stride, k_stride, v_stride, pos};
   return hip_status(hyq::launch_paged_append(*cache, *batch, *rope, x, static_cast<uint16_t*>(q_out),
@@ -735,6 +758,11 @@ HYQ_API int hyq_paged_attn(const hyq_pcache* cache, const hyq_pbatch* batch, con
   if (need > 0 && (!ws || ws_bytes < need))
     return fail(HYQ_EINVAL, "workspace too small: %zu bytes given, %zu needed", ws_bytes, need);
   if (!aligned16(ws)) return fail(HYQ_EINVAL, "the workspace must be aligned to 16 bytes");
+  const size_t n = (size_t)batch->T * cache->Hq * cache->D, out_bytes = n * (out_dtype ? 2 : 4);
+  if (overlaps(out, out_bytes, q, n * 2))
+    return fail(HYQ_EINVAL, "out must not overlap q (every split and the masses read it)");
+  if (need > 0 && (overlaps(ws, need, q, n * 2) || overlaps(ws, need, out, out_bytes)))
+    return fail(HYQ_EINVAL, "the workspace must not overlap q or out");
   return hip_status(hyq::launch_paged_attn(*cache, *batch, static_cast<const uint16_t*>(q),
                                            softmax_scale, mass, out, out_dtype, ws,
                                            static_cast<hipStream_t>(stream)),

@@ -9,6 +9,7 @@ import paper_2608_27875_amd as hyq
 
 EINVAL, EUNSUP = hyq.HYQ_EINVAL, hyq.HYQ_EUNSUPPORTED
 FAKE = 0x1000   # never dereferenced: the calls fail first
+OUT, WS = 1 << 40, 1 << 44   # outputs and a workspace elsewhere
 
 
 @pytest.fixture(scope="module")
@@ -62,11 +63,11 @@ BAD_ROPE = [
 ]
 
 
-def append(lib, c=None, b=None, r=None, q=FAKE, qs=1024, k=FAKE, ks=256, v=FAKE, vs=256, pos=FAKE, out=FAKE):
+def append(lib, c=None, b=None, r=None, q=FAKE, qs=1024, k=FAKE, ks=256, v=FAKE, vs=256, pos=FAKE, out=OUT):
     return lib.hyq_paged_append(c or cache(), b or batch(), r or rope(), q, qs, k, ks, v, vs, pos, out, None)
 
 
-def attn(lib, c=None, b=None, q=FAKE, scale=0.1, mass=0, out=FAKE, odt=0, ws=FAKE, wsb=1 << 40):
+def attn(lib, c=None, b=None, q=FAKE, scale=0.1, mass=0, out=OUT, odt=0, ws=WS, wsb=1 << 40):
     return lib.hyq_paged_attn(c or cache(), b or batch(), q, ctypes.c_float(scale), mass, out, odt, ws,
                               ctypes.c_size_t(wsb), None)
 
@@ -77,8 +78,8 @@ def evict(lib, c=None, B=2, lens=FAKE, table=FAKE, max_pages=8, max_len=100, bud
                          new_pages, keep, new_lens, None)
 
 
-def norm_rope(lib, s=None, r=None, q=FAKE, qs=1024, k=FAKE, ks=256, v=FAKE, vs=256, pos=FAKE, Q=FAKE,
-              K=FAKE, V=FAKE):
+def norm_rope(lib, s=None, r=None, q=FAKE, qs=1024, k=FAKE, ks=256, v=FAKE, vs=256, pos=FAKE, Q=OUT,
+              K=OUT << 1, V=OUT << 2):
     s = s or hyq.Shape(B=1, Hq=8, Hkv=2, L=4)
     return lib.hyq_norm_rope(s.c(), r or rope(), q, qs, k, ks, v, vs, pos, Q, K, V, None)
 
@@ -136,6 +137,30 @@ def test_bad_norm_rope_shapes(lib):
                                 dict(ws=None, mass=1), dict(wsb=15, mass=1), dict(ws=FAKE + 8, mass=1)])
 def test_bad_attention_arguments(lib, kw):
     assert attn(lib, **kw) == EINVAL
+
+
+APART = 6 * 8 * 256    # bytes of q's rows in `batch`: T = 6, 8 heads
+
+
+@pytest.mark.parametrize("kw", [dict(out=FAKE), dict(out=FAKE + APART - 16), dict(q=OUT + 2 * APART - 16),
+                                dict(odt=1, out=FAKE), dict(mass=1, ws=FAKE), dict(mass=1, ws=OUT + 16)])
+def test_attention_outputs_apart_from_inputs(lib, kw):
+    assert attn(lib, **kw) == EINVAL
+    assert "overlap" in hyq.hyq_last_error()
+
+
+@pytest.mark.parametrize("kw", [dict(out=FAKE), dict(k=OUT + APART - 16), dict(v=OUT),
+                                dict(q=OUT - 5 * 4096 * 2, qs=4096), dict(k=OUT - 16, ks=4096)])
+def test_appended_queries_apart_from_inputs(lib, kw):
+    assert append(lib, **kw) == EINVAL
+    assert "overlap" in hyq.hyq_last_error()
+
+
+@pytest.mark.parametrize("kw", [dict(Q=FAKE), dict(K=FAKE), dict(V=FAKE), dict(q=OUT + 4 * 8 * 256 - 16),
+                                dict(v=(OUT << 1) - 3 * 8192, vs=4096), dict(k=(OUT << 2) + 16)])
+def test_norm_rope_outputs_apart_from_inputs(lib, kw):
+    assert norm_rope(lib, **kw) == EINVAL
+    assert "overlap" in hyq.hyq_last_error()
 
 
 def test_mass_needs_a_buffer(lib):
