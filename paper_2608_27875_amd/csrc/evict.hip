@@ -3,10 +3,11 @@
 // the largest mass, in ascending order, in new pages.
 //
 // Two launches.  The selection (one workgroup per KV head) reads 4 bytes a
-// slot: the budget-th largest order key by three radix passes over a
-// histogram in LDS, the keys held in registers, then the kept slots in order
-// by lane scans.  It is bound by latency (the passes follow each other): 18.6 us
-// for 32k slots, 10 us for 8k.  The move copies the kept rows, 16 lanes to a row:
+// slot: the budget-th largest order key by radix passes over a histogram in LDS,
+// three at most (usually two: the budget then ends with a bin), the keys held in
+// registers, then the kept slots in order by lane scans.  It is bound by latency:
+// 17 us for 32k slots, of which 8 until the keys are there, 2 and 1.5 in the two
+// passes, 3 to place; 10 us for 8k.  The move copies the kept rows, 16 lanes to a row:
 // HBM, 16 x 8 x 1000 E4M3 rows in 15.3 us (4.7 TB/s).
 #include "paged_dev.h"
 
@@ -58,11 +59,11 @@ evict_select_kernel(EvictArgs a) {
   // equal bins of a wave are added one after the other
   __shared__ uint4 hist[kBins];
   __shared__ uint32_t wsum[kSelWaves];
-  __shared__ uint32_t found[2];   // bin, count above it
+  __shared__ uint32_t found[3];   // bin, keys above it, keys in it
   uint32_t* const h32 = reinterpret_cast<uint32_t*>(hist);
   const int bj = blockIdx.x, b = bj / a.g.Hkv, j = bj - b * a.g.Hkv;
   const int n = slots_of(a, b), m = min(n, a.budget);
-  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+  const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
   int32_t* keep = a.keep + (size_t)bj * a.budget;
   for (int i = m + tid; i < a.budget; i += kSelThreads) keep[i] = HYQ_KQ_POS_PAD;
   if (j == 0 && tid == 0) a.new_lens[b] = m;
@@ -72,37 +73,48 @@ evict_select_kernel(EvictArgs a) {
   }
   const int groups = MORE ? (n + C * kChunk - 1) / (C * kChunk) : 1;
   uint32_t key[C * 4];
-  auto load = [&](int grp) {
+  float4 f[C];
+  int p[C];
+  auto fetch = [&](int grp) {
     const int n0 = (grp * kSelWaves + w) * C * 256 + lane * 4;
-    float4 f[C];
-    int p[C];
 #pragma unroll
     for (int c = 0; c < C; ++c) {   // 4 slots from a multiple of 4 on: one page
       p[c] = page_of(a.g, b, n0 + 256 * c);
       f[c] = *reinterpret_cast<const float4*>(a.mass + pool_row(a.g, max(p[c], 0), j, n0 + 256 * c));
     }
+  };
+  auto convert = [&](int grp) {
 #pragma unroll
     for (int c = 0; c < C; ++c) {
+      const int first = ((grp * kSelWaves + w) * C + c) * 256;   // of the wave's slots
       const float x[4] = {f[c].x, f[c].y, f[c].z, f[c].w};
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int slot = n0 + 256 * c + e;
-        const uint32_t u = p[c] < 0 || x[e] != x[e] || slot >= n ? 0u : order_key(x[e]);
-        key[4 * c + e] = slot >= n - a.recent && slot < n ? 0xffffffffu : u;
+      for (int e = 0; e < 4; ++e) key[4 * c + e] = p[c] < 0 || x[e] != x[e] ? 0u : order_key(x[e]);
+      if (first + 256 > n - a.recent) {   // the same for the whole wave, rarely
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int slot = first + lane * 4 + e;
+          if (slot >= n - a.recent) key[4 * c + e] = slot < n ? 0xffffffffu : 0u;
+        }
       }
     }
   };
-  if (!MORE) load(0);
+  if (!MORE) fetch(0);
   // the m-th largest key, bits from the top; `left` of the keys that share the
   // bits found so far are still wanted
   uint32_t prefix = 0, left = (uint32_t)m;
   int shift = 32;
-  for (int pass = 0; pass < 3; ++pass) {
+  bool whole = false;   // all keys that share them are
+  for (int pass = 0; pass < 3 && !whole; ++pass) {
     const int bits = pass < 2 ? 11 : 10, below = shift - bits;
     for (int i = tid; i < kBins; i += kSelThreads) hist[i] = make_uint4(0u, 0u, 0u, 0u);
     __syncthreads();
+    if (!MORE && pass == 0) convert(0);
     for (int grp = 0; grp < groups; ++grp) {
-      if (MORE) load(grp);
+      if (MORE) {
+        fetch(grp);
+        convert(grp);
+      }
 #pragma unroll
       for (int e = 0; e < 4 * C; ++e)
         if (pass == 0 || (key[e] >> shift) == prefix)
@@ -122,20 +134,73 @@ evict_select_kernel(EvictArgs a) {
       const bool second = before + c0 < left;
       found[0] = (uint32_t)(kBins - 1 - 2 * tid) - (second ? 1u : 0u);
       found[1] = before + (second ? c0 : 0u);
+      found[2] = second ? c1 : c0;
     }
     __syncthreads();
-    prefix = (prefix << bits) | found[0];
-    left -= found[1];
+    prefix = (prefix << bits) | (uint32_t)__builtin_amdgcn_readfirstlane((int)found[0]);
+    left -= (uint32_t)__builtin_amdgcn_readfirstlane((int)found[1]);
+    whole = (uint32_t)__builtin_amdgcn_readfirstlane((int)found[2]) == left;
     shift = below;
   }
-  // a kept slot's place is the number of larger keys before it plus the equal
-  // ones before it, of which the first `left` are kept
+  // Counts of the lane's four slots per chunk, three chunks to a word (a wave's
+  // are at most 256), are scanned over the lanes.
+  constexpr int kWords = (C + 2) / 3;
+  auto field = [](uint32_t x, int c) { return (x >> (10 * (c % 3))) & 1023u; };
+  // Usually all keys that share the threshold's bits are kept: places are then
+  // counts of keys that are not below it.
+  if (whole) {
+    uint32_t least = prefix << shift;
+    uint32_t kept0 = 0;   // of all groups before
+    for (int grp = 0; grp < groups; ++grp) {
+      if (MORE) {
+        fetch(grp);
+        convert(grp);
+      }
+      uint32_t cnt[kWords] = {}, scan[kWords], kept = 0, before[C];
+#pragma unroll
+      for (int c = 0; c < C; ++c) {
+        uint32_t own = 0;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) own += key[4 * c + e] >= least;
+        cnt[c / 3] += own << (10 * (c % 3));
+      }
+#pragma unroll
+      for (int x = 0; x < kWords; ++x) scan[x] = wave_scan(cnt[x]);
+#pragma unroll
+      for (int c = 0; c < C; ++c) {
+        before[c] = kept + field(scan[c / 3] - cnt[c / 3], c);
+        kept += field(__builtin_amdgcn_readlane((int)scan[c / 3], 63), c);
+      }
+      if (lane == 0) wsum[w] = kept;
+      __syncthreads();
+      uint32_t lower = kept0;
+#pragma unroll
+      for (int x = 0; x < kSelWaves; ++x) {
+        const uint32_t v = wsum[x];
+        lower += x < w ? v : 0u;
+        kept0 += v;
+      }
+      const int n0 = (grp * kSelWaves + w) * C * 256 + lane * 4;
+      asm volatile("" : "+s"(least));   // compare again: the masks of all keys do not fit
+#pragma unroll
+      for (int c = 0; c < C; ++c) {
+        uint32_t at = lower + before[c];
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (key[4 * c + e] >= least) keep[at++] = n0 + 256 * c + e;
+      }
+      __syncthreads();
+    }
+    return;
+  }
+  // Otherwise (all 32 bits are found) a kept slot's place is the number of larger
+  // keys before it plus the equal ones before it, of which the first `left` are kept.
   uint32_t gt0 = 0, eq0 = 0;   // of all groups before
   for (int grp = 0; grp < groups; ++grp) {
-    if (MORE) load(grp);
-    // counts of the lane's four slots per chunk, three chunks to a word (a
-    // wave's are at most 256), scanned over the lanes
-    constexpr int kWords = (C + 2) / 3;
+    if (MORE) {
+      fetch(grp);
+      convert(grp);
+    }
     uint32_t gw[kWords] = {}, ew[kWords] = {}, gs[kWords], es[kWords];
 #pragma unroll
     for (int c = 0; c < C; ++c)
@@ -152,11 +217,10 @@ evict_select_kernel(EvictArgs a) {
     }
 #pragma unroll
     for (int c = 0; c < C; ++c) {
-      const int sh = 10 * (c % 3);
-      before_g[c] = all_g + (((gs[c / 3] - gw[c / 3]) >> sh) & 1023u);
-      before_e[c] = all_e + (((es[c / 3] - ew[c / 3]) >> sh) & 1023u);
-      all_g += ((uint32_t)__builtin_amdgcn_readlane((int)gs[c / 3], 63) >> sh) & 1023u;
-      all_e += ((uint32_t)__builtin_amdgcn_readlane((int)es[c / 3], 63) >> sh) & 1023u;
+      before_g[c] = all_g + field(gs[c / 3] - gw[c / 3], c);
+      before_e[c] = all_e + field(es[c / 3] - ew[c / 3], c);
+      all_g += field(__builtin_amdgcn_readlane((int)gs[c / 3], 63), c);
+      all_e += field(__builtin_amdgcn_readlane((int)es[c / 3], 63), c);
     }
     if (lane == 0) wsum[w] = all_g | all_e << 16;   // a group holds at most 2^15 slots
     __syncthreads();
@@ -168,6 +232,7 @@ evict_select_kernel(EvictArgs a) {
       all += v;
     }
     const int n0 = (grp * kSelWaves + w) * C * 256 + lane * 4;
+    asm volatile("" : "+s"(prefix));
 #pragma unroll
     for (int c = 0; c < C; ++c) {
       uint32_t gt = gt0 + (lower & 0xffffu) + before_g[c], eq = eq0 + (lower >> 16) + before_e[c];

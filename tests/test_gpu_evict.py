@@ -23,6 +23,8 @@ CASES = [
     ([20000], 1, 16, "bf16", 4000, 128, 0, "odd"),
     ([40000, 33000], 1, 64, "int8", 2000, 100, 0, "wide"),  # keys read again for every pass
     ([5000], 1, 64, "bf16", 4999, 1, 40000, "few values"),
+    ([400, 800], 2, 16, "bf16", 75, 0, 0, "classes"),       # three whole classes; one and a half
+    ([33600, 400], 1, 16, "fp8", 4200, 0, 0, "classes"),    # two whole ones, keys read again
 ]
 
 
@@ -31,6 +33,8 @@ def masses(rng, kind, shape):
         return np.where(rng.random(shape) < 0.5, 0.0, -0.0).astype(np.float32)
     if kind == "few values":
         return rng.integers(0, 5, shape).astype(np.float32) / 4
+    if kind == "classes":   # every 16 slots hold each of 16 powers of two once
+        return np.broadcast_to(2.0 ** (np.arange(shape[-1]) % 16 - 8), shape).astype(np.float32)
     if kind == "odd":
         x = rng.standard_normal(shape).astype(np.float32)
         r = rng.random(shape)
