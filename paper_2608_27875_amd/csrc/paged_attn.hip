@@ -55,11 +55,15 @@ struct AttnArgs {
   int few_max;         // sequences of at most so many rows go to the few-row kernel
   int S_few, S_many;   // splits of the keys in the two kernels
   int join_few;        // whether the few-row kernel leaves partials
-  float* part;         // partial sums over a split's keys [S][T][Hq][kHeadDim]
-  float2* part_ml;     // their (max, sum) [T][Hq][S]
-  int S_part;          // S of the two: the larger of the splits
-  float* logit;        // few rows with mass: [B][Hkv][logit_rows][logit_stride]
-  int logit_rows, logit_stride;
+  // Partial sums over a split's keys and their (max, sum): of chunks
+  // [S_many][T][Hq][kHeadDim] and [T][Hq][S_many], of few rows
+  // [S_few][B][Hkv][few_rows][kHeadDim] and [B][Hkv][few_rows][S_few] (by token they
+  // would grow with the chunks of a mixed batch).
+  float *many_part, *few_part;
+  float2 *many_ml, *few_ml;
+  int few_rows;
+  float* logit;        // few rows with mass: [B][Hkv][few_rows][logit_stride]
+  int logit_stride;
   uint32_t inv_g;      // ceil(2^32 / g) (g > 1): r / g for the rows of a step
   float2* stat;        // many rows with mass: (max, 1 / sum) of every query row [T][Hq]
 };
@@ -328,7 +332,7 @@ paged_few_kernel(AttnArgs a) {
   const int nu = (sq.n_kv + kUnit - 1) / kUnit, nw = a.S_few * kFewWaves, gw = sp * kFewWaves + w;
   const int first = (int)((int64_t)gw * nu / nw), end = (int)((int64_t)(gw + 1) * nu / nw);
   const int* trow = a.g.table + (size_t)b * a.g.max_pages;
-  float* lg = a.logit ? a.logit + ((size_t)((size_t)b * a.g.Hkv + j) * a.logit_rows + hl) * a.logit_stride + 8 * G
+  float* lg = a.logit ? a.logit + ((size_t)((size_t)b * a.g.Hkv + j) * a.few_rows + hl) * a.logit_stride + 8 * G
                       : nullptr;
   if (lg && hl >= rows) lg = nullptr;
   Unit<FMT> r0, r1;
@@ -388,8 +392,9 @@ paged_few_kernel(AttnArgs a) {
     const int ii = rw / a.g.g;
     const size_t row = (size_t)(sq.t0 + ii) * a.g.Hq + (size_t)j * a.g.g + (rw - ii * a.g.g);
     if (a.join_few) {
-      *reinterpret_cast<v4f*>(a.part + ((size_t)sp * a.g.T * a.g.Hq + row) * kHeadDim + ch) = acc;
-      if (ch == 0) a.part_ml[row * a.S_part + sp] = make_float2(M, sum);
+      const size_t heads = (size_t)a.g.B * a.g.Hkv, at = ((size_t)b * a.g.Hkv + j) * a.few_rows + rw;
+      *reinterpret_cast<v4f*>(a.few_part + (sp * heads * a.few_rows + at) * kHeadDim + ch) = acc;
+      if (ch == 0) a.few_ml[at * a.S_few + sp] = make_float2(M, sum);
     } else {
       store4(a, row, ch, acc * (sum > 0.0f ? 1.0f / sum : 0.0f));
     }
@@ -708,14 +713,14 @@ paged_many_kernel(AttnArgs a, const int32_t* __restrict__ table, int tiles) {
   l += __shfl_xor(l, 32, 64);
   if (r_mine >= rows) return;
   if (a.S_many > 1) {
-    float* dst = a.part + ((size_t)sp * a.g.T * a.g.Hq + qrow) * kHeadDim;
+    float* dst = a.many_part + ((size_t)sp * a.g.T * a.g.Hq + qrow) * kHeadDim;
 #pragma unroll
     for (int d = 0; d < 4; ++d)
 #pragma unroll
       for (int e = 0; e < 4; ++e)
         *reinterpret_cast<v4f*>(dst + d * 32 + e * 8 + hf * 4) =
             v4f{acc[d][4 * e], acc[d][4 * e + 1], acc[d][4 * e + 2], acc[d][4 * e + 3]};
-    if (hf == 0) a.part_ml[(size_t)qrow * a.S_part + sp] = make_float2(m, l);
+    if (hf == 0) a.many_ml[(size_t)qrow * a.S_many + sp] = make_float2(m, l);
   } else {
     const float inv = l > 0.0f ? 1.0f / l : 0.0f;
 #pragma unroll
@@ -737,17 +742,17 @@ constexpr int kFinishThreads = 256;   // few rows: up to kFewSplits
 constexpr int kStatThreads = kFinishThreads / kFewRows;   // threads that join a row's maximum and sum
 constexpr int kMassKeys = kFinishThreads * 4;   // keys of a mass workgroup of the few-row path
 
-// Row `row` (token * Hq + head) of the output from its S partials: shares of
-// them, 32 lanes of 4 channels each, joined through LDS.
+// Row `row` (token * Hq + head) of the output from its S partials, `stride` floats
+// apart, and their (max, sum): shares of them, 32 lanes of 4 channels each, joined
+// through LDS.
 template <int THREADS>
-__device__ __forceinline__ void join_row(const AttnArgs& a, size_t row, int S) {
+__device__ __forceinline__ void join_row(const AttnArgs& a, size_t row, const float* part, size_t stride,
+                                         const float2* mls, int S) {
   constexpr int kShares = THREADS / 32;
   __shared__ v4f x_acc[kShares][32];
   __shared__ float x_m[kShares], x_l[kShares];
   const int c4 = threadIdx.x & 31, ph = threadIdx.x >> 5;
-  const float* base = a.part + row * kHeadDim + c4 * 4;
-  const size_t stride = (size_t)a.g.T * a.g.Hq * kHeadDim;
-  const float2* mls = a.part_ml + row * a.S_part;
+  const float* base = part + c4 * 4;
   float M = kFloor, L = 0.0f;
   v4f acc = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll 4
@@ -788,7 +793,9 @@ paged_join_kernel(AttnArgs a) {
   if (b < 0) return;
   const Seq sq = seq_of(a.g, b);
   if (t - sq.t0 >= sq.n_new || sq.n_new * a.g.g <= a.few_max) return;
-  join_row<kJoinThreads>(a, blockIdx.x, a.S_many);
+  const size_t row = blockIdx.x;
+  join_row<kJoinThreads>(a, row, a.many_part + row * kHeadDim, (size_t)a.g.T * a.g.Hq * kHeadDim,
+                         a.many_ml + row * a.S_many, a.S_many);
 }
 
 // After the few-row kernel (one launch for both, 16 us at 16 x 32k slots; 33 as
@@ -804,12 +811,15 @@ paged_few_finish_kernel(AttnArgs a) {
   const Seq sq = seq_of(a.g, b);
   const int rows = sq.n_new * a.g.g;
   if (rows == 0 || rows > a.few_max) return;
-  auto row_of = [&](int r) {
-    const int i = r / a.g.g;
-    return (size_t)(sq.t0 + i) * a.g.Hq + (size_t)j * a.g.g + (r - i * a.g.g);
-  };
+  const size_t first = ((size_t)b * a.g.Hkv + j) * a.few_rows;   // of the head's partials
   if (blockIdx.y < kFewRows) {
-    if ((int)blockIdx.y < rows) join_row<kFinishThreads>(a, row_of(blockIdx.y), a.S_few);
+    if ((int)blockIdx.y < rows) {
+      const size_t at = first + blockIdx.y;
+      const int i = (int)blockIdx.y / a.g.g;
+      join_row<kFinishThreads>(a, (size_t)(sq.t0 + i) * a.g.Hq + (size_t)j * a.g.g + (blockIdx.y - i * a.g.g),
+                               a.few_part + at * kHeadDim, (size_t)a.g.B * a.g.Hkv * a.few_rows * kHeadDim,
+                               a.few_ml + at * a.S_few, a.S_few);
+    }
     return;
   }
   const int key = (blockIdx.y - kFewRows) * kMassKeys + (int)threadIdx.x * 4;
@@ -817,7 +827,7 @@ paged_few_finish_kernel(AttnArgs a) {
   __shared__ float2 st[kFewRows];
   if ((int)threadIdx.x < rows * kStatThreads) {
     const int r = threadIdx.x / kStatThreads;
-    const float2* mls = a.part_ml + row_of(r) * a.S_part;
+    const float2* mls = a.few_ml + (first + r) * a.S_few;
     float M = kFloor, L = 0.0f;
 #pragma unroll 8
     for (int s = threadIdx.x % kStatThreads; s < a.S_few; s += kStatThreads) {
@@ -837,7 +847,7 @@ paged_few_finish_kernel(AttnArgs a) {
   }
   __syncthreads();
   if (key >= sq.n_kv) return;
-  const float* lg = a.logit + ((size_t)b * a.g.Hkv + j) * a.logit_rows * a.logit_stride + key;
+  const float* lg = a.logit + first * a.logit_stride + key;
   v4f sum = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll 4
   for (int r = 0; r < rows; ++r) {
@@ -979,10 +989,9 @@ struct Plan {
   int waves;           // of a workgroup of the many-row kernel (32 rows each)
   int row_tiles;       // row tiles of a sequence there
   int64_t n_kv;        // bound on a sequence's slots
-  int logit_rows, logit_stride;
-  int S_part;          // splits whose partials are kept
-  size_t part, ml, logit, stat;   // workspace bytes
-  size_t total() const { return part + ml + logit + stat; }
+  int few_rows, logit_stride;
+  size_t many_part, many_ml, few_part, few_ml, logit, stat;   // workspace bytes
+  size_t total() const { return many_part + many_ml + few_part + few_ml + logit + stat; }
 };
 
 size_t up256(size_t x) { return (x + 255) & ~(size_t)255; }
@@ -1015,17 +1024,21 @@ Plan plan_of(const hyq_pcache& c, const hyq_pbatch& b, int mass) {
   p.S_many = (int)std::max<int64_t>(1, std::min({(p.waves == 4 ? 512 : 256) / wg, (ktiles + 7) / 8, (int64_t)64}));
   p.join_few = p.few && (p.S_few > 1 || mass);
   p.join_many = p.many && p.S_many > 1;
-  p.S_part = std::max(p.join_few ? p.S_few : 0, p.join_many ? p.S_many : 0);
   const size_t qrows = (size_t)b.T * c.Hq;
-  p.part = up256((size_t)p.S_part * qrows * kHeadDim * 4);
-  p.ml = up256((size_t)p.S_part * qrows * sizeof(float2));
-  if (mass) {
-    if (p.many) p.stat = up256(qrows * sizeof(float2));
-    if (p.few) {
-      p.logit_rows = p.many ? kFewRows : rows;
-      p.logit_stride = (int)(units * kUnit);
-      p.logit = up256((size_t)heads * p.logit_rows * p.logit_stride * 4);
-    }
+  p.few_rows = p.many ? kFewRows : rows;
+  const size_t frows = (size_t)heads * p.few_rows;
+  if (p.join_many) {
+    p.many_part = up256(p.S_many * qrows * kHeadDim * 4);
+    p.many_ml = up256(p.S_many * qrows * sizeof(float2));
+  }
+  if (p.join_few) {
+    p.few_part = up256(p.S_few * frows * kHeadDim * 4);
+    p.few_ml = up256(p.S_few * frows * sizeof(float2));
+  }
+  if (mass && p.many) p.stat = up256(qrows * sizeof(float2));
+  if (mass && p.few) {
+    p.logit_stride = (int)(units * kUnit);
+    p.logit = up256(frows * p.logit_stride * 4);
   }
   return p;
 }
@@ -1083,16 +1096,19 @@ hipError_t launch_paged_attn(const hyq_pcache& c, const hyq_pbatch& b, const uin
   a.S_many = p.S_many;
   a.join_few = p.join_few;
   char* w = static_cast<char*>(ws);
-  if (p.part) a.part = reinterpret_cast<float*>(w);
-  w += p.part;
-  if (p.ml) a.part_ml = reinterpret_cast<float2*>(w);
-  w += p.ml;
-  a.S_part = p.S_part;
-  if (p.logit) a.logit = reinterpret_cast<float*>(w);
-  w += p.logit;
-  a.logit_rows = p.logit_rows;
+  auto take = [&w](size_t n) {
+    char* at = n ? w : nullptr;
+    w += n;
+    return at;
+  };
+  a.many_part = reinterpret_cast<float*>(take(p.many_part));
+  a.many_ml = reinterpret_cast<float2*>(take(p.many_ml));
+  a.few_part = reinterpret_cast<float*>(take(p.few_part));
+  a.few_ml = reinterpret_cast<float2*>(take(p.few_ml));
+  a.logit = reinterpret_cast<float*>(take(p.logit));
+  a.stat = reinterpret_cast<float2*>(take(p.stat));
+  a.few_rows = p.few_rows;
   a.logit_stride = p.logit_stride;
-  if (p.stat) a.stat = reinterpret_cast<float2*>(w);
   if (c.bits_kv == 16) return launch<kBf16>(p, a, st);
   if (c.kv_format == HYQ_FMT_FP8) return launch<HYQ_FMT_FP8>(p, a, st);
   return launch<HYQ_FMT_INT>(p, a, st);

@@ -231,6 +231,16 @@ def test_workspace_grows_with_the_batch(lib, B, Hq, Hkv, max_new):
             last = max(last, n[1].value) if T >= B else last
 
 
+def test_workspace_of_a_mixed_batch(lib):
+    """The splits of a single token do not multiply the rows of the chunk beside it:
+    one KV head's partials of 16 rows in 256 splits, 520 bytes each."""
+    c, _ = hyq.hyq_pcache_init(8, 1, 32, 1000)
+    n = ctypes.c_size_t()
+    b = hyq._PBatch(2, 4096, 4095, 1 << 17, 1 << 16, None, None, None)
+    assert lib.hyq_paged_ws_bytes(c, b, 0, ctypes.byref(n)) == 0
+    assert n.value <= 2 * 16 * 256 * 520 + 4096
+
+
 def test_binding_checks():
     """The binding refuses tensors of other shapes, types and places."""
     import torch
