@@ -418,7 +418,8 @@ typedef struct hyq_rope {
 
 /*
  * For every row x of q (weight w = q_weight) and k (k_weight):
- *   y = x * w / sqrt(mean(x^2) + eps)        (y = x where w is NULL)
+ *   y = x * w / sqrt(mean(x^2) + eps)        (y = x where w is NULL; y = 0
+ *                                             for a row of zeros, eps = 0 too)
  *   the pair (a, c) of frequency f becomes (a cos - c sin, c cos + a sin) of
  *   the angle pos * inv_freq[f]
  * in float32 (the angle in float64), rounded to bf16 once; v is copied.

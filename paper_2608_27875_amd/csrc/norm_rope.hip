@@ -14,7 +14,8 @@
 //     pos * inv_freq is taken in float64 and reduced to a turn there (a float32
 //     angle is off by radians from positions of a few million on), the sine
 //     and cosine in float32;
-//   - one rounding: everything between the loads and the stores is float32.
+//   - one rounding: everything between the loads and the stores is float32
+//     (float64 for rows whose squares leave its range).
 // 8192 tokens of 48 rows take 33.4 us (6.0 TB/s), 16 tokens 3.5 us, 2106 tokens
 // of a ragged batch into E4M3 pages 15.0 us (3.2 TB/s; latency).  Loading a
 // lane's rows of all passes up front was slower (40.8 us at 8192 tokens): the
@@ -70,6 +71,30 @@ __device__ __forceinline__ void widen8(const uint4& w, float (&x)[8]) {
     x[2 * e] = bf16_lo(u[e]);
     x[2 * e + 1] = bf16_hi(u[e]);
   }
+}
+
+// Whether a row's mean square (with eps) is below 2^-100 or infinite: squares of
+// its entries may then have left float32's range.
+__device__ __forceinline__ bool squares_lost(float ms) {
+  constexpr uint32_t kLeast = 0x0d800000u, kInf = 0x7f800000u;   // bits of 2^-100 and infinity
+  return __float_as_uint(ms) - kLeast >= kInf - kLeast;
+}
+
+// The norm of such a row in float64, which holds the square of every float.  A
+// row of zeros stays zero without eps too: a dead head or padding must not put
+// NaN into a page.  The row's 16 lanes call it together.  Never taken in earnest;
+// to ask costs an append of 2106 tokens 0.4 us of 14.
+__device__ __forceinline__ void norm_wide(float (&x)[8], const uint4& raw, const float (&w)[8], float eps) {
+  widen8(raw, x);
+  double ss = 0.0;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) ss += (double)x[e] * (double)x[e];
+#pragma unroll
+  for (int o = 8; o >= 1; o >>= 1) ss += __shfl_xor(ss, o, 16);
+  const double ms = ss * (1.0 / kHeadDim) + (double)eps;
+  const double inv = ms > 0.0 ? 1.0 / sqrt(ms) : 0.0;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) x[e] = (float)((double)x[e] * inv * (double)w[e]);
 }
 
 __device__ __forceinline__ uint32_t pack2(float a, float b) {
@@ -160,11 +185,15 @@ norm_rope_kernel(RopeArgs a, int passes) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) ss = __builtin_fmaf(x[e], x[e], ss);
         ss = sum16(ss);
-        const float inv = 1.0f / sqrtf(ss * (1.0f / kHeadDim) + a.eps);
+        const float ms = ss * (1.0f / kHeadDim) + a.eps;
+        const float inv = 1.0f / sqrtf(ms);
         float wf[8];
         widen8(wr, wf);
 #pragma unroll
         for (int e = 0; e < 8; ++e) x[e] *= inv * wf[e];
+        if (__builtin_expect(__ballot(squares_lost(ms)) != 0, 0)) {
+          if (squares_lost(ms)) norm_wide(x, raw, wf, a.eps);
+        }
       }
       if (a.interleaved) {
         if (!is_v && sub * 8 < a.rot) {
