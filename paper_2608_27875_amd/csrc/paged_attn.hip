@@ -21,7 +21,10 @@
 // launch joins them, which also turns the logits into masses.
 #include "paged_dev.h"
 
+#include <float.h>
+
 #include <algorithm>
+#include <type_traits>
 
 namespace hyq {
 namespace {
@@ -40,7 +43,7 @@ constexpr int kFewSplits = 256;      // most splits of a sequence's keys there
 constexpr int kKeyTile = 64;         // keys of a tile of the many-row kernel
 constexpr float kLazy = 8.0f;        // rescale only when the maximum grows by more than 2^8
 constexpr float kNever = 3.0e38f;    // the "maximum" of a row that sees nothing: exp2(z - it) is 0
-constexpr float kFloor = -1.0e30f;   // start of a running maximum (finite: exp2 of -inf - it is 0)
+constexpr float kFloor = -FLT_MAX;   // start of a running maximum (finite: exp2 of -inf - it is 0)
 
 struct AttnArgs {
   PagedGeom g;
@@ -67,6 +70,16 @@ struct AttnArgs {
   uint32_t inv_g;      // ceil(2^32 / g) (g > 1): r / g for the rows of a step
   float2* stat;        // many rows with mass: (max, 1 / sum) of every query row [T][Hq]
 };
+
+// How far score z (times c) is above the reference m of its row, which is such a
+// product rounded alike: the largest scores get weight 1 at any size.  One fused
+// operation would leave up to half a step of m, and weights of 0 or infinity from
+// scores of 2^31 on.
+__device__ __forceinline__ float above(float z, float c, float m) {
+#pragma clang fp contract(off)
+  const float zc = z * c;
+  return zc - m;
+}
 
 // Token of row r of a KV head's rows: r / g.  Exact for r < 2^29 (the quotient
 // is too large by less than r / 2^32 < 1 / g, g <= 8).
@@ -258,7 +271,7 @@ __device__ __forceinline__ void few_unit(FewState& st, const Unit<FMT>& r, const
   uint32_t hi[8], lo[8];
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
-    float p = __builtin_amdgcn_exp2f(__builtin_fmaf(y[e], c, -st.m));
+    float p = __builtin_amdgcn_exp2f(above(y[e], c, st.m));
     st.l += p;
     if constexpr (FMT != kBf16) p *= e < there ? r.vs[e >> 2][e & 3] : 0.0f;
     hi[e] = __float_as_uint(p) & 0xffff0000u;
@@ -546,7 +559,12 @@ __device__ __forceinline__ v8bf read_v(const v4u* vt, int lane_part, int o, int 
 // PFLOP/s, a large matrix product reaches 1.22); 3 x 2k over 6011 int8 slots, 40
 // heads over 8: 840 us (0.83 PFLOP/s).  Power sets the clock there: running two
 // groups of waves half a tile apart cut cycles but not time.
+//
+// Weights come from one fused operation each; where a row of the wave has its
+// reference beyond 2^16 (up to there the exponent differs from `above` by 2^-8 at
+// most), they are taken once more by `above`, in every tile.
 constexpr float kFarSum = 0x1p16f;
+constexpr float kFarScore = 0x1p16f;
 
 template <int FMT, int NW>
 __global__ void __launch_bounds__(NW * 64, 2)
@@ -584,6 +602,7 @@ paged_many_kernel(AttnArgs a, const int32_t* __restrict__ table, int tiles) {
 #pragma unroll
     for (int e = 0; e < 16; ++e) acc[d][e] = 0.0f;
   float m = kFloor, l = 0.0f;
+  bool far = false;   // some row of the wave has its reference beyond kFarScore
 
   if (first < end) {
     const int kg = threadIdx.x >> 4, chunk = threadIdx.x & 15;
@@ -669,7 +688,7 @@ paged_many_kernel(AttnArgs a, const int32_t* __restrict__ table, int tiles) {
       asm volatile("" : "+v"(pcur[0]), "+v"(pcur[1]), "+v"(pcur[2]), "+v"(pcur[3]), "+v"(ps), "+v"(ps1));
       ps += ps1;
       __builtin_amdgcn_s_setprio(0);
-      if (tile == first || __ballot(!(ps <= kFarSum))) {
+      if (tile == first || far || __ballot(!(ps <= kFarSum))) {
         float top = -INFINITY;
 #pragma unroll
         for (int x = 0; x < 2; ++x)
@@ -684,15 +703,22 @@ paged_many_kernel(AttnArgs a, const int32_t* __restrict__ table, int tiles) {
           for (int e = 0; e < 16; ++e) acc[d][e] *= f;
         l *= f;
         m = mnew;
+        far = __ballot(m > kFloor && fabsf(m) > kFarScore) != 0;
         ps = 0.0f;
+        auto weights = [&](auto fused) {
 #pragma unroll
-        for (int x = 0; x < 2; ++x)
+          for (int x = 0; x < 2; ++x)
 #pragma unroll
-          for (int e = 0; e < 16; ++e) {
-            const float pw = __builtin_amdgcn_exp2f(__builtin_fmaf(s[x][e], factor(kb, x, e >> 2)[e & 3], -m));
-            ps += pw;
-            pcur[x * 2 + (e >> 3)][e & 7] = (__bf16)(pw * value_scale(kb, x, e >> 2)[e & 3]);
-          }
+            for (int e = 0; e < 16; ++e) {
+              const float c = factor(kb, x, e >> 2)[e & 3];
+              const float d = decltype(fused)::value ? __builtin_fmaf(s[x][e], c, -m) : above(s[x][e], c, m);
+              const float pw = __builtin_amdgcn_exp2f(d);
+              ps += pw;
+              pcur[x * 2 + (e >> 3)][e & 7] = (__bf16)(pw * value_scale(kb, x, e >> 2)[e & 3]);
+            }
+        };
+        if (far) weights(std::false_type{});
+        else weights(std::true_type{});
       }
       l += ps;
       // V of this tile: its buffer was last read before the barrier too
@@ -855,7 +881,7 @@ paged_few_finish_kernel(AttnArgs a) {
     const float2 ml = st[r];
 #pragma unroll
     for (int e = 0; e < 4; ++e)
-      sum[e] = __builtin_fmaf(__builtin_amdgcn_exp2f(__builtin_fmaf(z[e], a.c_log2, -ml.x)), ml.y, sum[e]);
+      sum[e] = __builtin_fmaf(__builtin_amdgcn_exp2f(above(z[e], a.c_log2, ml.x)), ml.y, sum[e]);
   }
   const int p = page_of(a.g, b, key);
   if (p < 0) return;
@@ -959,7 +985,7 @@ paged_many_mass_kernel(AttnArgs a) {
       }
 #pragma unroll
       for (int e = 0; e < 16; ++e)
-        sum[e] = __builtin_fmaf(__builtin_amdgcn_exp2f(__builtin_fmaf(s[e], kse[e], -ml.x)), ml.y, sum[e]);
+        sum[e] = __builtin_fmaf(__builtin_amdgcn_exp2f(above(s[e], kse[e], ml.x)), ml.y, sum[e]);
     }
     store((tile + 1) & 1);
   }
