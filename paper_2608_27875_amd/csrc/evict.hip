@@ -65,7 +65,8 @@ evict_select_kernel(EvictArgs a) {
   const int n = slots_of(a, b), m = min(n, a.budget);
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
   int32_t* keep = a.keep + (size_t)bj * a.budget;
-  for (int i = m + tid; i < a.budget; i += kSelThreads) keep[i] = HYQ_KQ_POS_PAD;
+  // unsigned: i may pass 2^31 where a budget is near it
+  for (uint32_t i = (uint32_t)(m + tid); i < (uint32_t)a.budget; i += kSelThreads) keep[i] = HYQ_KQ_POS_PAD;
   if (j == 0 && tid == 0) a.new_lens[b] = m;
   if (n <= a.budget) {
     for (int i = tid; i < n; i += kSelThreads) keep[i] = i;
