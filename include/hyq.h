@@ -429,6 +429,7 @@ typedef struct hyq_rope {
  * with Hkv heads (three slices of one packed projection, or three tensors).
  * pos: int32 [B*L], any value.  Q [B][Hq][L][D], K and V [B][Hkv][L][D] bf16,
  * not overlapping the inputs.  v and V may be NULL together; so may k and K.
+ * At most 2^24 - 1 tokens and 2^30 head rows (B * L * (Hq + 2 Hkv)).
  * With L = 1 the outputs are the rows of hyq_decode_append / hyq_decode_attn.
  */
 HYQ_API int hyq_norm_rope(const hyq_shape* shape, const hyq_rope* rope, const void* q,

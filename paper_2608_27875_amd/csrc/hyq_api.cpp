@@ -651,10 +651,10 @@ HYQ_API int hyq_norm_rope(const hyq_shape* shape, const hyq_rope* rope, const vo
     return rc;
   if (!aligned16(Q) || !aligned16(K) || !aligned16(V))
     return fail(HYQ_EINVAL, "Q, K and V must be aligned to 16 bytes");
-  if ((int64_t)shape->B * shape->L * (shape->Hq + 2 * shape->Hkv) > kMaxRows)
-    return fail(HYQ_EUNSUPPORTED, "%lld token rows in one call not supported",
-                (long long)shape->B * shape->L);
+  // a workgroup of 256 per token; head rows are counted in 32 bits (2^30 are 512 GiB)
   const int64_t T = (int64_t)shape->B * shape->L;
+  if (T >= (int64_t)1 << 24 || T * ((int64_t)shape->Hq + 2 * (int64_t)shape->Hkv) > (int64_t)1 << 30)
+    return fail(HYQ_EUNSUPPORTED, "%lld token rows in one call not supported", (long long)T);
   const struct {
     const char* name;
     const void* p;

@@ -94,3 +94,30 @@ def test_appended_rows_of_any_size(fmt):
         half = s[:, None] * (0.5 if kind == "int" else 2.0 ** -10) + (0.0 if kind == "int" else 2.0 ** -4) * np.abs(want)
         assert np.all(np.abs(got - want) <= half * (1 + 2.0 ** -10) + 2.0 ** -17 * np.abs(want).max(-1, keepdims=True))
     assert np.isfinite(got).all() and np.all(got[0] == 0)
+
+
+def test_more_rows_than_24_bits_count():
+    """17.5 million head rows, byte offsets beyond 2^32: values are copied, and
+    queries and keys are right at tokens all over the call."""
+    import torch
+    B, Hq, Hkv, L = 2, 8, 1, 875011
+    T, H = B * L, Hq + 2 * Hkv
+    g = torch.Generator(device="cuda").manual_seed(1)
+    x = torch.empty((T, H, D), dtype=torch.bfloat16, device="cuda").normal_(generator=g)
+    q, k, v = x.split([Hq, Hkv, Hkv], dim=1)
+    w = pc.bits(np.random.default_rng(6), D)
+    rope, f = rope_of(D, False, w, w)
+    pos = torch.arange(T, device="cuda", dtype=torch.int32)
+    Q, K, V = (torch.full((B, h, L, D), float("nan"), dtype=torch.bfloat16, device="cuda") for h in (Hq, Hkv, Hkv))
+    hyq.hyq_norm_rope(hyq.Shape(B=B, Hq=Hq, Hkv=Hkv, L=L), rope, q, k, v, pos, Q, K, V)
+    torch.cuda.synchronize()
+    assert torch.equal(V.view(torch.int16).view(T, D), v.contiguous().view(torch.int16).view(T, D))
+    assert bool(torch.isfinite(Q).all()) and bool(torch.isfinite(K).all())
+    at = np.unique(np.concatenate([[0, 1, L - 1, L, T - 1], np.random.default_rng(7).integers(0, T, 60)]))
+    rows = pc.host(x[torch.from_numpy(at).cuda()])
+    got_q = pc.host(Q.transpose(1, 2).reshape(T, Hq, D)[torch.from_numpy(at).cuda()])
+    got_k = pc.host(K.transpose(1, 2).reshape(T, Hkv, D)[torch.from_numpy(at).cuda()])
+    close(got_q, po.norm_rope(rows[:, :Hq], po.bf16(w), at, f, D), "Q")
+    close(got_k, po.norm_rope(rows[:, Hq:Hq + Hkv], po.bf16(w), at, f, D), "K")
+    del x, q, k, v, Q, K, V
+    torch.cuda.empty_cache()
