@@ -458,6 +458,9 @@ typedef struct hyq_pcache_sizes {
   size_t mass_bytes;     /* of mass                                                */
 } hyq_pcache_sizes;
 
+/* Most head rows of a step: T * (Hq + 2 Hkv). */
+#define HYQ_PAGED_MAX_ROWS (1 << 24)
+
 /* One step of B sequences with T token rows in all: tokens [cu_new[b],
    cu_new[b+1]) are the new ones of sequence b (none is fine), which go to its
    slots lens[b], lens[b] + 1, ...  Rows from cu_new[B] on belong to nobody:
@@ -499,7 +502,11 @@ HYQ_API int hyq_paged_append(const hyq_pcache* cache, const hyq_pbatch* batch,
 #define HYQ_MASS_SET  2   /* cache.mass = the weights of this call                 */
 
 /* Workspace of hyq_paged_attn for this cache and these bounds (host only; the
-   device arrays of the batch are not read and may be NULL).  0: none needed. */
+   device arrays of the batch are not read and may be NULL).  0: none needed.
+   One for T token rows serves fewer.  With masses it holds a float32 logit for
+   every slot up to max_len + max_new of every sequence and KV head, in as many
+   rows as few new tokens can have: max_new * Hq/Hkv, or 16 where that is more
+   (256 sequences of 32768 slots with 8 KV heads and a chunk among them: 4.3 GB). */
 HYQ_API int hyq_paged_ws_bytes(const hyq_pcache* cache, const hyq_pbatch* batch, int32_t mass,
                                size_t* bytes);
 

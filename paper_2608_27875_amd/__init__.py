@@ -28,6 +28,7 @@ WIN_FIXED, WIN_BAND = 0, 1    # hyq_shape.window_mode
 SEL_PROXY, SEL_COLMASS = 0, 1  # hyq_shape.selector
 MASS_NONE, MASS_ADD, MASS_SET = 0, 1, 2   # what hyq_paged_attn does with the weights
 DECODE_WS = 64                # HYQ_DECODE_WS: staging buffer capacity
+PAGED_MAX_ROWS = 1 << 24      # HYQ_PAGED_MAX_ROWS: token rows * (Hq + 2 Hkv) of a step
 EXPORTED = ("hyq_sizes_for", "hyq_select_vertical", "hyq_quantize", "hyq_attn_prefill",
             "hyq_prefill", "hyq_strerror", "hyq_last_error", "hyq_dcache_init", "hyq_freeze",
             "hyq_decode_append", "hyq_decode_attn", "hyq_decode_attn_noalloc", "hyq_norm_rope",
@@ -702,9 +703,12 @@ def hyq_paged_append(cache: PagedCache, batch: PagedBatch, rope: Rope, q, k, v, 
 def hyq_paged_ws_bytes(cache: PagedCache, batch: PagedBatch, mass: bool = False,
                        T: int | None = None) -> int:
     """Workspace bytes of hyq_paged_attn within the batch's bounds, for T token
-    rows (default: B * max_new, the most there can be)."""
+    rows (default: B * max_new or the most that a step may have, whichever is
+    less; a smaller T needs no more)."""
     n = ctypes.c_size_t()
-    b = batch.of(batch.B * batch.c.max_new if T is None else T)
+    if T is None:
+        T = min(batch.B * batch.c.max_new, PAGED_MAX_ROWS // (cache.c.Hq + 2 * cache.c.Hkv))
+    b = batch.of(T)
     _check(lib().hyq_paged_ws_bytes(ctypes.byref(cache.c), ctypes.byref(b),
                                     MASS_SET if mass else MASS_NONE, ctypes.byref(n)))
     return n.value

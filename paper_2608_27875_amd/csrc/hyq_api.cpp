@@ -312,9 +312,9 @@ int check_pcache(const hyq_pcache* c) {
   return HYQ_OK;
 }
 
-// Bounds of a batch (its device arrays are checked by the calls that read them).
+// Bounds of a batch (its device arrays are checked by the calls that read them;
+// whether its workgroups fit a grid, by those that launch them).
 constexpr int64_t kMaxSlots = (int64_t)1 << 22;   // of one sequence
-constexpr int64_t kMaxRows = (int64_t)1 << 24;    // query rows (tokens * heads) of one step
 int check_pbatch(const hyq_pcache* c, const hyq_pbatch* b) {
   if (!b) return fail(HYQ_EINVAL, "batch is NULL");
   if (b->B < 1 || b->T < 0 || b->max_new < 0 || b->max_len < 0 || b->max_pages < 1)
@@ -323,10 +323,14 @@ int check_pbatch(const hyq_pcache* c, const hyq_pbatch* b) {
   if ((int64_t)b->max_len + b->max_new > kMaxSlots)
     return fail(HYQ_EUNSUPPORTED, "sequences of up to %lld slots not supported (at most %lld)",
                 (long long)b->max_len + b->max_new, (long long)kMaxSlots);
-  if ((int64_t)b->T * (c->Hq + 2 * c->Hkv) > kMaxRows)
+  if ((int64_t)b->T * (c->Hq + 2 * c->Hkv) > HYQ_PAGED_MAX_ROWS)
     return fail(HYQ_EUNSUPPORTED, "%d token rows in one step not supported", b->T);
   if ((int64_t)b->B * c->Hkv > 32768)
     return fail(HYQ_EUNSUPPORTED, "%d sequences in one step not supported", b->B);
+  return HYQ_OK;
+}
+
+int check_pbatch_grid(const hyq_pcache* c, const hyq_pbatch* b) {
   if (!hyq::paged_grid_fits(*c, *b))
     return fail(HYQ_EUNSUPPORTED, "%d sequences of up to %d new tokens in one step not supported", b->B,
                 b->max_new);
@@ -706,7 +710,8 @@ HYQ_API int hyq_paged_append(const hyq_pcache* cache, const hyq_pbatch* batch,
                              const int32_t* pos, void* q_out, void* stream) {
   int rc = check_pcache(cache);
   if (rc) return rc;
-  if ((rc = check_pbatch(cache, batch)) || (rc = check_rope(rope))) return rc;
+  if ((rc = check_pbatch(cache, batch)) || (rc = check_pbatch_grid(cache, batch)) || (rc = check_rope(rope)))
+    return rc;
   if (batch->T == 0 || batch->max_new == 0) return ok();
   if ((rc = check_pbatch_arrays(batch))) return rc;
   if (!k || !v || !pos) return fail(HYQ_EINVAL, "k, v and pos must be non-NULL");
@@ -743,7 +748,8 @@ HYQ_API int hyq_paged_attn(const hyq_pcache* cache, const hyq_pbatch* batch, con
                            void* ws, size_t ws_bytes, void* stream) {
   int rc = check_pcache(cache);
   if (rc) return rc;
-  if ((rc = check_pbatch(cache, batch)) || (rc = check_mass(mass))) return rc;
+  if ((rc = check_pbatch(cache, batch)) || (rc = check_pbatch_grid(cache, batch)) || (rc = check_mass(mass)))
+    return rc;
   if (mass != HYQ_MASS_NONE && !cache->mass)
     return fail(HYQ_EINVAL, "the cache has no mass buffer to collect the weights in");
   if (out_dtype != 0 && out_dtype != 1)
