@@ -403,7 +403,9 @@ HYQ_API int hyq_decode_attn_noalloc(const hyq_dcache* cache, const void* q, floa
  * sees and whose rows are not written; lengths are taken as at most the
  * bounds given with them.  No such value makes a kernel leave its buffers.
  * Slots behind a sequence may hold anything (NaN too); the rows of its own
- * slots must be finite.  Buffers must be aligned to 16 bytes.
+ * slots must be finite.  Buffers must be aligned to 16 bytes, and what a call
+ * writes must lie apart from all that it reads and from what else it writes
+ * (refused with HYQ_EINVAL otherwise).
  * ==================================================================== */
 
 typedef struct hyq_rope {
@@ -428,7 +430,7 @@ typedef struct hyq_rope {
  * elements from token to token (a multiple of 8, >= Hq * D), k and v the same
  * with Hkv heads (three slices of one packed projection, or three tensors).
  * pos: int32 [B*L], any value.  Q [B][Hq][L][D], K and V [B][Hkv][L][D] bf16,
- * not overlapping the inputs.  v and V may be NULL together; so may k and K.
+ * apart from the inputs and each other.  v and V may be NULL together; so may k and K.
  * At most 2^24 - 1 tokens and 2^30 head rows (B * L * (Hq + 2 Hkv)).
  * With L = 1 the outputs are the rows of hyq_decode_append / hyq_decode_attn.
  */
@@ -488,8 +490,7 @@ HYQ_API int hyq_pcache_init(int32_t Hq, int32_t Hkv, int32_t D, int32_t page, in
  * bf16, k and v rows into their slots (codes are taken of the float32 values,
  * not of bf16 ones); mass, where there is one, is 0 in those slots.
  * q, k, v: bf16 rows [T][heads][D] with strides as for hyq_norm_rope; pos
- * int32 [T].  q_out must not overlap the inputs; q and q_out may be NULL together
- * (keys and values only).
+ * int32 [T].  q and q_out may be NULL together (keys and values only).
  * lens is not changed: hyq_paged_attn of the same step takes the same batch.
  */
 HYQ_API int hyq_paged_append(const hyq_pcache* cache, const hyq_pbatch* batch,
@@ -503,10 +504,10 @@ HYQ_API int hyq_paged_append(const hyq_pcache* cache, const hyq_pbatch* batch,
 
 /* Workspace of hyq_paged_attn for this cache and these bounds (host only; the
    device arrays of the batch are not read and may be NULL).  0: none needed.
-   One for T token rows serves fewer.  With masses it holds a float32 logit for
-   every slot up to max_len + max_new of every sequence and KV head, in as many
-   rows as few new tokens can have: max_new * Hq/Hkv, or 16 where that is more
-   (256 sequences of 32768 slots with 8 KV heads and a chunk among them: 4.3 GB). */
+   One for T token rows serves fewer.  With masses it holds a float32 logit of
+   every slot up to max_len + max_new in min(max_new * Hq/Hkv, 16) rows of every
+   sequence and KV head (256 sequences of 32768 slots with 8 KV heads and a chunk
+   among them: 4.3 GB).                                                       */
 HYQ_API int hyq_paged_ws_bytes(const hyq_pcache* cache, const hyq_pbatch* batch, int32_t mass,
                                size_t* bytes);
 
@@ -520,8 +521,7 @@ HYQ_API int hyq_paged_ws_bytes(const hyq_pcache* cache, const hyq_pbatch* batch,
  * With mass, for every slot n < lens[b] + new of a sequence with new tokens:
  *   mass[b][j][n] (+)= sum over its new tokens i and the g heads of group j of
  *                      the weight w_n / sum w that they give n.
- * q: bf16 [T][Hq][D]; out: [T][Hq][D], float32 (out_dtype 0) or bf16 (1); out,
- * q and ws must not overlap.
+ * q: bf16 [T][Hq][D]; out: [T][Hq][D], float32 (out_dtype 0) or bf16 (1).
  * Precision: bf16 products (8-bit codes are exact in bf16, their scales are
  * applied in float32), float32 sums; the weights enter the products with V as
  * a high + low bf16 pair where a sequence has at most 16 query rows per KV

@@ -274,9 +274,32 @@ int check_rows(const char* name, const void* p, int64_t stride, int heads, int D
   return HYQ_OK;
 }
 
-// Whether n bytes at out overlap rows of a norm_rope / append call.
-bool overlaps_rows(const void* out, size_t n, const void* p, int64_t stride, int heads, int D, int64_t T) {
-  return out && p && overlaps(out, n, p, ((size_t)(T - 1) * stride + (size_t)heads * D) * 2);
+// A buffer of a paged call; one without an address or without bytes is not there.
+struct Span {
+  const char* name;
+  const void* p;
+  size_t n;
+};
+Span rows_span(const char* name, const void* p, int64_t stride, int heads, int D, int64_t T) {
+  return {name, p, ((size_t)(T - 1) * stride + (size_t)heads * D) * 2};
+}
+Span weight_span(const char* name, const void* p) { return {name, p, hyq::kHeadDim * 2}; }
+
+// What a call writes must lie apart from what it reads and from what else it
+// writes: workgroups read and write in any order, and an eviction's kernels take
+// the kept slots, which they use as indexes, from memory.
+template <size_t N, size_t M>
+int check_apart(const Span (&outs)[N], const Span (&ins)[M]) {
+  auto clash = [](const Span& a, const Span& b) { return a.p && b.p && a.n && b.n && overlaps(a.p, a.n, b.p, b.n); };
+  for (size_t i = 0; i < N; ++i) {
+    const Span* other = nullptr;
+    for (const Span& x : ins)
+      if (clash(outs[i], x)) other = &x;
+    for (size_t j = i + 1; j < N; ++j)
+      if (clash(outs[i], outs[j])) other = &outs[j];
+    if (other) return fail(HYQ_EINVAL, "%s must not overlap %s", outs[i].name, other->name);
+  }
+  return HYQ_OK;
 }
 
 // Geometry of a paged cache, without its buffers.
@@ -298,6 +321,11 @@ int check_pcache_geometry(const hyq_pcache* c) {
   if (c->Hq / c->Hkv > 8)
     return fail(HYQ_EUNSUPPORTED, "GQA group size %d not supported (at most 8)", c->Hq / c->Hkv);
   return HYQ_OK;
+}
+
+hyq_pcache_sizes pcache_sizes(const hyq_pcache& c) {
+  const size_t rows = (size_t)c.n_pages * c.Hkv * c.page;
+  return {rows * c.D * (c.bits_kv / 8), c.bits_kv == 8 ? rows * 4 : 0, rows * 4};
 }
 
 int check_pcache(const hyq_pcache* c) {
@@ -659,18 +687,14 @@ HYQ_API int hyq_norm_rope(const hyq_shape* shape, const hyq_rope* rope, const vo
   const int64_t T = (int64_t)shape->B * shape->L;
   if (T >= (int64_t)1 << 24 || T * ((int64_t)shape->Hq + 2 * (int64_t)shape->Hkv) > (int64_t)1 << 30)
     return fail(HYQ_EUNSUPPORTED, "%lld token rows in one call not supported", (long long)T);
-  const struct {
-    const char* name;
-    const void* p;
-    int heads;
-  } outs[] = {{"Q", Q, shape->Hq}, {"K", K, shape->Hkv}, {"V", V, shape->Hkv}};
-  for (const auto& o : outs) {
-    const size_t n = (size_t)T * o.heads * shape->D * 2;
-    if (overlaps_rows(o.p, n, q, q_stride, shape->Hq, shape->D, T) ||
-        overlaps_rows(o.p, n, k, k_stride, shape->Hkv, shape->D, T) ||
-        overlaps_rows(o.p, n, v, v_stride, shape->Hkv, shape->D, T))
-      return fail(HYQ_EINVAL, "%s must not overlap the inputs (rows go to other places)", o.name);
-  }
+  const int D = shape->D;
+  const size_t q_bytes = (size_t)T * shape->Hq * D * 2, kv_bytes = (size_t)T * shape->Hkv * D * 2;
+  const Span outs[] = {{"Q", Q, q_bytes}, {"K", K, kv_bytes}, {"V", V, kv_bytes}};
+  const Span ins[] = {rows_span("q", q, q_stride, shape->Hq, D, T), rows_span("k", k, k_stride, shape->Hkv, D, T),
+                      rows_span("v", v, v_stride, shape->Hkv, D, T), {"pos", pos, (size_t)T * 4},
+                      weight_span("q_weight", rope->q_weight), weight_span("k_weight", rope->k_weight),
+                      {"inv_freq", rope->inv_freq, (size_t)rope->rot_dim * 2}};
+  if ((rc = check_apart(outs, ins))) return rc;
   const hyq::RopeRows x = {static_cast<const uint16_t*>(q), static_cast<const uint16_t*>(k),
                            static_cast<const uint16_t*>(v), q_stride, k_stride, v_stride, pos};
   return hip_status(hyq::launch_norm_rope(*shape, *rope, x, static_cast<uint16_t*>(Q),
@@ -695,12 +719,7 @@ HYQ_API int hyq_pcache_init(int32_t Hq, int32_t Hkv, int32_t D, int32_t page, in
   const int rc = check_pcache_geometry(&c);
   if (rc) return rc;
   *cache = c;
-  if (sizes) {
-    const size_t rows = (size_t)n_pages * Hkv * page;
-    sizes->kv_bytes = rows * D * (bits_kv / 8);
-    sizes->scale_bytes = bits_kv == 8 ? rows * 4 : 0;
-    sizes->mass_bytes = rows * 4;
-  }
+  if (sizes) *sizes = pcache_sizes(c);
   return ok();
 }
 
@@ -721,11 +740,20 @@ HYQ_API int hyq_paged_append(const hyq_pcache* cache, const hyq_pbatch* batch,
       (rc = check_rows("v", v, v_stride, cache->Hkv, cache->D)))
     return rc;
   if (!aligned16(q_out)) return fail(HYQ_EINVAL, "q_out must be aligned to 16 bytes");
-  const size_t q_bytes = (size_t)batch->T * cache->Hq * cache->D * 2;
-  if (overlaps_rows(q_out, q_bytes, q, q_stride, cache->Hq, cache->D, batch->T) ||
-      overlaps_rows(q_out, q_bytes, k, k_stride, cache->Hkv, cache->D, batch->T) ||
-      overlaps_rows(q_out, q_bytes, v, v_stride, cache->Hkv, cache->D, batch->T))
-    return fail(HYQ_EINVAL, "q_out must not overlap the inputs");
+  const int D = cache->D;
+  const int64_t T = batch->T;
+  const hyq_pcache_sizes z = pcache_sizes(*cache);
+  const Span outs[] = {{"q_out", q_out, (size_t)T * cache->Hq * D * 2}, {"the cache's k", cache->k, z.kv_bytes},
+                       {"the cache's v", cache->v, z.kv_bytes}, {"the cache's k_scale", cache->k_scale, z.scale_bytes},
+                       {"the cache's v_scale", cache->v_scale, z.scale_bytes},
+                       {"the cache's mass", cache->mass, z.mass_bytes}};
+  const Span ins[] = {rows_span("q", q, q_stride, cache->Hq, D, T), rows_span("k", k, k_stride, cache->Hkv, D, T),
+                      rows_span("v", v, v_stride, cache->Hkv, D, T), {"pos", pos, (size_t)T * 4},
+                      weight_span("q_weight", rope->q_weight), weight_span("k_weight", rope->k_weight),
+                      {"inv_freq", rope->inv_freq, (size_t)rope->rot_dim * 2},
+                      {"cu_new", batch->cu_new, ((size_t)batch->B + 1) * 4}, {"lens", batch->lens, (size_t)batch->B * 4},
+                      {"table", batch->table, (size_t)batch->B * batch->max_pages * 4}};
+  if ((rc = check_apart(outs, ins))) return rc;
   const hyq::RopeRows x = {static_cast<const uint16_t*>(q), static_cast<const uint16_t*>(k),
                            static_cast<const uint16_t*>(v), q_stride, k_stride, v_stride, pos};
   return hip_status(hyq::launch_paged_append(*cache, *batch, *rope, x, static_cast<uint16_t*>(q_out),
@@ -764,11 +792,17 @@ HYQ_API int hyq_paged_attn(const hyq_pcache* cache, const hyq_pbatch* batch, con
   if (need > 0 && (!ws || ws_bytes < need))
     return fail(HYQ_EINVAL, "workspace too small: %zu bytes given, %zu needed", ws_bytes, need);
   if (!aligned16(ws)) return fail(HYQ_EINVAL, "the workspace must be aligned to 16 bytes");
-  const size_t n = (size_t)batch->T * cache->Hq * cache->D, out_bytes = n * (out_dtype ? 2 : 4);
-  if (overlaps(out, out_bytes, q, n * 2))
-    return fail(HYQ_EINVAL, "out must not overlap q (every split and the masses read it)");
-  if (need > 0 && (overlaps(ws, need, q, n * 2) || overlaps(ws, need, out, out_bytes)))
-    return fail(HYQ_EINVAL, "the workspace must not overlap q or out");
+  const size_t n = (size_t)batch->T * cache->Hq * cache->D;
+  const hyq_pcache_sizes z = pcache_sizes(*cache);
+  // k and v may be one buffer here: they are only read
+  const Span outs[] = {{"out", out, n * (out_dtype ? 2 : 4)}, {"the workspace", ws, need},
+                       {"the cache's mass", cache->mass, mass == HYQ_MASS_NONE ? 0 : z.mass_bytes}};
+  const Span ins[] = {{"q", q, n * 2}, {"the cache's k", cache->k, z.kv_bytes}, {"the cache's v", cache->v, z.kv_bytes},
+                      {"the cache's k_scale", cache->k_scale, z.scale_bytes},
+                      {"the cache's v_scale", cache->v_scale, z.scale_bytes},
+                      {"cu_new", batch->cu_new, ((size_t)batch->B + 1) * 4}, {"lens", batch->lens, (size_t)batch->B * 4},
+                      {"table", batch->table, (size_t)batch->B * batch->max_pages * 4}};
+  if ((rc = check_apart(outs, ins))) return rc;
   return hip_status(hyq::launch_paged_attn(*cache, *batch, static_cast<const uint16_t*>(q),
                                            softmax_scale, mass, out, out_dtype, ws,
                                            static_cast<hipStream_t>(stream)),
@@ -797,8 +831,15 @@ HYQ_API int hyq_evict(const hyq_pcache* cache, int32_t B, const int32_t* lens,
     return fail(HYQ_EUNSUPPORTED, "%d sequences in one call not supported", B);
   if (!lens || !table || !new_table || !keep || !new_lens)
     return fail(HYQ_EINVAL, "lens, table, new_table, keep and new_lens must be non-NULL");
-  if (overlaps(lens, (size_t)B * 4, new_lens, (size_t)B * 4))
-    return fail(HYQ_EINVAL, "new_lens must not overlap lens (every KV head reads it)");
+  const hyq_pcache_sizes z = pcache_sizes(*cache);
+  const Span outs[] = {{"keep", keep, (size_t)B * cache->Hkv * budget * 4}, {"new_lens", new_lens, (size_t)B * 4},
+                       {"the cache's k", cache->k, z.kv_bytes}, {"the cache's v", cache->v, z.kv_bytes},
+                       {"the cache's k_scale", cache->k_scale, z.scale_bytes},
+                       {"the cache's v_scale", cache->v_scale, z.scale_bytes},
+                       {"the cache's mass", cache->mass, z.mass_bytes}};
+  const Span ins[] = {{"lens", lens, (size_t)B * 4}, {"table", table, (size_t)B * max_pages * 4},
+                      {"new_table", new_table, (size_t)B * new_pages * 4}};
+  if ((rc = check_apart(outs, ins))) return rc;
   return hip_status(hyq::launch_evict(*cache, B, lens, table, max_pages, max_len, budget, recent,
                                       new_table, new_pages, keep, new_lens,
                                       static_cast<hipStream_t>(stream)),
