@@ -515,9 +515,9 @@ HYQ_API int hyq_paged_ws_bytes(const hyq_pcache* cache, const hyq_pbatch* batch,
  * For new token i of sequence b, query head h and its KV head j:
  *   z_n = softmax_scale * <q, K[n]> over the slots n <= lens[b] + i,
  *   out = sum_n w_n V[n] / sum_n w_n, w_n = exp(z_n - max z);
- * a row that sees no key (all holes) gives 0.  Scores may be of any size that
- * float32 holds, log2(e) times them too.  The new tokens' rows must be in their
- * slots (hyq_paged_append).
+ * a row that sees no key (all holes) gives 0.  Scores (and softmax_scale) may be
+ * of any size that float32 holds, log2(e) times them too.  The new tokens' rows
+ * must be in their slots (hyq_paged_append).
  * With mass, for every slot n < lens[b] + new of a sequence with new tokens:
  *   mass[b][j][n] (+)= sum over its new tokens i and the g heads of group j of
  *                      the weight w_n / sum w that they give n.

@@ -782,8 +782,8 @@ HYQ_API int hyq_paged_attn(const hyq_pcache* cache, const hyq_pbatch* batch, con
     return fail(HYQ_EINVAL, "the cache has no mass buffer to collect the weights in");
   if (out_dtype != 0 && out_dtype != 1)
     return fail(HYQ_EINVAL, "out_dtype must be 0 (float32) or 1 (bf16), got %d", out_dtype);
-  if (!(softmax_scale > 0.0f) || softmax_scale == INFINITY)
-    return fail(HYQ_EINVAL, "softmax_scale must be positive and finite");
+  if (!(softmax_scale > 0.0f) || softmax_scale * 1.44269504088896340736f == INFINITY)
+    return fail(HYQ_EINVAL, "softmax_scale must be positive, and finite times log2(e)");
   if (batch->T == 0 || batch->max_new == 0) return ok();
   if ((rc = check_pbatch_arrays(batch))) return rc;
   if (!q || !out) return fail(HYQ_EINVAL, "q and out must be non-NULL");
