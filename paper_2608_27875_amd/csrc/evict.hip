@@ -7,8 +7,10 @@
 // three at most (usually two: the budget then ends with a bin), the keys held in
 // registers, then the kept slots in order by lane scans.  It is bound by latency:
 // 17 us for 32k slots, of which 8 until the keys are there, 2 and 1.5 in the two
-// passes, 3 to place; 10 us for 8k.  The move copies the kept rows, 16 lanes to a row:
-// HBM, 16 x 8 x 1000 E4M3 rows in 15.3 us (4.7 TB/s).
+// passes, 3 to place; 10 us for 8k.  Above 32768 slots every pass and the placement
+// read the keys again: 131072 slots to 2048 take 62 to 64 us with the move.  The
+// move copies the kept rows, 16 lanes to a row: HBM, 16 x 8 x 1000 E4M3 rows in
+// 15 us (4.6 TB/s).
 #include "paged_dev.h"
 
 namespace hyq {

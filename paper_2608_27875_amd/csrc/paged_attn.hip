@@ -266,8 +266,8 @@ __device__ __forceinline__ void few_unit(FewState& st, const Unit<FMT>& r, const
     st.m = mnew;
   }
   const int there = r.gone ? 0 : n_kv - key0;   // of the lane's 8 keys, those somebody owns
-  // weights as a high + low bf16 pair (2^-17 relative): the kernel waits for
-  // memory, the second product is free
+  // weights as a high (truncated, 8 bits) + low (rounded) bf16 pair, 2^-16
+  // relative: the kernel waits for memory, the second product is free
   uint32_t hi[8], lo[8];
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
@@ -312,9 +312,9 @@ __device__ __forceinline__ void store4(const AttnArgs& a, size_t row, int ch, v4
 // Workgroup (b, s, j) (j fastest: the heads of a sequence go to different
 // XCDs, the splits of one head to one): its 4 waves take even shares of the
 // units, the next unit's loads in flight beside the one being computed; their
-// states are joined in LDS.  16 sequences of 32k slots, 32 heads over 8: 348 us
-// with the logits written (5.0 TB/s; a large copy reaches 5.2), 32 of 8k in E4M3
-// pages with 40 heads 82 us (5.1 TB/s).
+// states are joined in LDS.  16 sequences of 32k slots, 32 heads over 8: 348 to
+// 352 us with the logits written (4.9 TB/s; a large copy moves 4.8 to 5.2, the
+// norms 5.6), 32 of 8k in E4M3 pages with 40 heads 82 to 85 us (4.9 to 5.1 TB/s).
 template <int FMT>
 __global__ void __launch_bounds__(kFewThreads, 2)
 paged_few_kernel(AttnArgs a) {
@@ -555,10 +555,16 @@ __device__ __forceinline__ v8bf read_v(const v4u* vt, int lane_part, int o, int 
 // at any size, so the reference moves only when a lane's weights of a tile sum
 // to more than 2^16 (which leaves the accumulators their range).
 //
-// 512 tokens over 32256 slots, 32 heads over 8, bf16: 276 us with the join (0.99
-// PFLOP/s, a large matrix product reaches 1.22); 3 x 2k over 6011 int8 slots, 40
-// heads over 8: 840 us (0.83 PFLOP/s).  Power sets the clock there: running two
-// groups of waves half a tile apart cut cycles but not time.
+// Weights (times a value row's scale with codes) are rounded to bf16, the type of
+// the products; the row sum keeps them as they are.  Outputs in bf16 are then
+// 0.0024 off (relative, of normal values), 0.0017 by their own rounding alone.  A
+// high + low pair as above would make 48 products of 32 a tile where products are
+// the bound.
+//
+// 512 tokens over 32256 slots, 32 heads over 8, bf16: 272 us and 11 to join (1.0
+// PFLOP/s, a large matrix product reaches 1.18 to 1.22); 3 x 2k over 6011 int8
+// slots, 40 heads over 8: 844 us (0.82 PFLOP/s).  Power sets the clock there:
+// running two groups of waves half a tile apart cut cycles but not time.
 //
 // Weights come from one fused operation each; where a row of the wave has its
 // reference beyond 2^16 (up to there the exponent differs from `above` by 2^-8 at
@@ -824,7 +830,7 @@ paged_join_kernel(AttnArgs a) {
                          a.many_ml + row * a.S_many, a.S_many);
 }
 
-// After the few-row kernel (one launch for both, 16 us at 16 x 32k slots; 33 as
+// After the few-row kernel (one launch for both, 15 us at 16 x 32k slots; 33 as
 // two): workgroups (b, j, y) with y < kFewRows join query row y; the others
 // (with masses) take 1024 keys each: the maximum and the sum of every row from
 // the partials, then the weights from the stored logits (4 keys a thread, rows in
@@ -899,8 +905,10 @@ paged_few_finish_kernel(AttnArgs a) {
 // known.  A wave owns 32 keys (their K rows stay in registers); the workgroup
 // walks the rows that see any of its 128 keys in tiles of 64, staged in LDS for
 // its four waves (chunk c of row r at c ^ (r & 15)), the next tile's loads in
-// flight.  512 tokens over 32256 slots, 32 heads over 8: 185 us, matrix cores busy
-// 36%, VALU 54%; with every row read from L2 by every wave it was 539.
+// flight.  512 tokens over 32256 slots, 32 heads over 8: 180 us, matrix cores busy
+// 35%, VALU 61%; with every row read from L2 by every wave it was 539.  Fused
+// exponents would save 5 us; taken only where no row of a half tile needs `above`,
+// the branch between the halves costs 6.
 constexpr int kMassThreads = 256, kMassTile = 64;
 
 template <int FMT>
@@ -1042,7 +1050,11 @@ Plan plan_of(const hyq_pcache& c, const hyq_pbatch& b, int mass) {
   // balance better: 2048 tokens from nothing 61 us against 66 with 256 rows, 8 x
   // 200 over 1000 slots 44 and 47, 4 x 8 over 9001 33 and 40.  Longer scans gain
   // more from eight waves sharing a tile's staging: 3 x 2k over 6011 int8 slots
-  // 839 and 966, 512 over 32k 276 and 295, 100 over 16k 50 and 52.
+  // 839 and 966, 512 over 32k 276 and 295, 100 over 16k 50 and 52.  Near the limit
+  // the two differ little (512 over 2500, 3400, 4000, 4600: four waves 50, 56, 59,
+  // 64, eight 50, 55, 58, 62; 8 x 200 over 4000 and 5000: 122, 149 and 123, 148),
+  // except where a step is large: 3 x 2k over 2500 slots 318 with eight and 328 with
+  // four, int8 372 and 418.
   p.waves = rows <= 128 || p.n_kv < 4096 ? 4 : 8;
   const int64_t wg = heads * ((rows + p.waves * 32 - 1) / (p.waves * 32));
   const int launched = std::min(b.max_new, b.T) * g;   // the grid (the splits go by max_new alone)
