@@ -527,8 +527,9 @@ HYQ_API int hyq_paged_ws_bytes(const hyq_pcache* cache, const hyq_pbatch* batch,
  * a high + low bf16 pair where a sequence has at most 16 query rows per KV
  * head (new tokens * Hq/Hkv; of a single sequence, max_new * Hq/Hkv), and as
  * bf16 where it has more (which adds an error of the size of a bf16 output's own
- * rounding: 0.0024 in all, relative, where that is 0.0017).  Values of up to 2^80
- * keep their weighted sums within float32.  Every result is the same from run to
+ * rounding: 0.0024 in all, relative, where that is 0.0017; up to 0.003 where few
+ * keys in 8-bit pages hold the weight).  Values of up to 2^80 keep their weighted
+ * sums within float32.  Every result is the same from run to
  * run: nothing is added atomically.
  * Allocates nothing and keeps no state; it can be captured in a HIP graph
  * (lens, tables and token counts may change between replays, within the
