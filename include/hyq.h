@@ -529,8 +529,8 @@ HYQ_API int hyq_paged_ws_bytes(const hyq_pcache* cache, const hyq_pbatch* batch,
  * bf16 where it has more (which adds an error of the size of a bf16 output's own
  * rounding: 0.0024 in all, relative, where that is 0.0017; up to 0.003 where few
  * keys in 8-bit pages hold the weight).  Values of up to 2^80 keep their weighted
- * sums within float32.  Every result is the same from run to
- * run: nothing is added atomically.
+ * sums within float32.  Every result is the same from run to run: nothing is
+ * added atomically.
  * Allocates nothing and keeps no state; it can be captured in a HIP graph
  * (lens, tables and token counts may change between replays, within the
  * bounds).  ws: scratch of hyq_paged_ws_bytes; calls that overlap need one each.

@@ -558,8 +558,8 @@ __device__ __forceinline__ v8bf read_v(const v4u* vt, int lane_part, int o, int 
 // Weights (times a value row's scale with codes) are rounded to bf16, the type of
 // the products; the row sum keeps them as they are.  Outputs in bf16 are then
 // 0.0024 off (relative, of normal values; up to 0.003 where few keys of 8-bit pages
-// hold the weight), 0.0017 by their own rounding alone.  A high + low pair as above would make 48 products of 32 a tile where products are
-// the bound.
+// hold the weight), 0.0017 by their own rounding alone.  A high + low pair as
+// above would make 48 products of 32 a tile where products are the bound.
 //
 // 512 tokens over 32256 slots, 32 heads over 8, bf16: 272 us and 11 to join (1.0
 // PFLOP/s, a large matrix product reaches 1.18 to 1.22); 3 x 2k over 6011 int8
